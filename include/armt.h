@@ -327,6 +327,70 @@ armt_status armt_lm_head(const armt_config *cfg, const void *hidden, int64_t n_r
 armt_status armt_lm_head_static(const armt_config *cfg, const void *hidden, int64_t n_rows, const void *final_gain,
                                 const void *w_lm, int32_t vocab, float *logits, void *hip_stream);
 
+/* ---- decoding: what a caller needs to go on from the last segment token by token, beside the single steps above: the new
+ * rows' keys and values into a paged cache, their attention over it, the selection of a beam search, and the reordering of its states.
+ * They allocate nothing, never wait, and can be recorded into a HIP graph; what changes from token to token (page table,
+ * lengths, rows per sequence) is read on the device.
+
+ * A paged cache of one layer's keys and values, of cfg->dtype.  A page holds page_len keys of every KV head, [Hkv][page_len][dh], page p at
+ * element p * page_stride of k and of v (0: dense; larger where the pages of several layers lie side by side).  pages[s][j] names the page of
+ * keys j * page_len .. of sequence s; an entry outside [0, n_pages) is no page: nothing is written to it and its keys do not
+ * exist.  Sequence s has lens[s] keys in front of a call's rows row_start[s] .. row_start[s + 1] - 1 (row_start rises from 0); row i of
+ * them is key lens[s] + i.  Rows behind row_start[n_seqs] belong to nobody and are left as they are.  lens[s] <= 2^30.
+ * Supported (else ARMT_ERR_UNSUPPORTED): page_len a power of two from 16 to 4096, head_dim a multiple of 4 up to 128 (bf16: 64 or
+ * 128), at most 65536 sequences; k, v, qkv, q, q_out and out and the strides of pages and of qkv multiples of 16 bytes. */
+typedef struct {
+  void *k, *v;               /* [n_pages] pages                                   */
+  const int32_t *pages;      /* [n_seqs][max_pages]                               */
+  const int32_t *lens;       /* [n_seqs]      keys in front of the call's rows    */
+  const int32_t *row_start;  /* [n_seqs + 1]                                      */
+  int32_t n_seqs, n_pages, page_len, max_pages;
+  int64_t page_stride;
+} armt_kv_cache;
+
+/* Rows of the fused projection into the cache, rotated on the way: q and k by their position as in armt_segment_attention, q_out [n_rows,
+ * H * dh] = R(p) q, key lens[s] + i = R(p) k, its value v.  qkv: rows [q heads | k heads | v heads], ld_qkv elements apart.
+ * positions [n_rows], or NULL for lens[s] + i (drafts of a tree that share a depth share a position).  A row whose key has no page gets its
+ * q_out all the same.  No workspace. */
+armt_status armt_kv_append(const armt_config *cfg, const armt_kv_cache *cache, const void *qkv, int64_t ld_qkv, int32_t n_rows,
+                           const int32_t *positions, void *q_out, void *hip_stream);
+
+/* Attention of the rows over the cache, their own keys (appended before) included: out[r][h] = softmax over the keys that row r sees
+ * (q[r][h] . k / sqrt(dh)) times v, grouped-query heads; q [n_rows, H * dh] rotated (q_out of armt_kv_append), out the same shape.
+ * Every row sees the lens[s] keys in front.  Of the call's own keys, row i sees key j iff bit j of tree[r] is set (a tree of
+ * drafted tokens: itself and its ancestors; at most 64 rows per sequence), or without a tree (NULL) iff j <= i (one token, or a chain).
+ * What a row does not see has no influence on it, not even a NaN; a row that sees no key is zero.  max_rows: at least the
+ * rows of any sequence (a longer sequence's further rows are left as they are).  Scores, probabilities' sums and outputs are
+ * accumulated in fp32; in bf16 the probabilities are rounded to bf16 for the second product.  The workspace is
+ * armt_kv_attention_workspace_bytes (0 = rejected) and 256-byte aligned; calls that may overlap need one each. */
+size_t armt_kv_attention_workspace_bytes(const armt_config *cfg, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t max_rows);
+armt_status armt_kv_attention(const armt_config *cfg, const armt_kv_cache *cache, const void *q, int32_t n_rows, int32_t max_rows,
+                              const uint64_t *tree, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* One step of a beam search: of all continuations (beam b, token v) of a sequence, with score scores[b] + logits[b][v] - log sum exp
+ * logits[b], the n_out best, best first; among equal ones (equal logits of one beam, equal scores of two) the lowest b * vocab + v first.
+ * logits [n_seqs * n_beams] rows ld_logits apart (fp32, as armt_lm_head writes them), scores [n_seqs, n_beams]; out_scores,
+ * out_parents (beam), out_tokens [n_seqs, n_out].  A logit of -inf bans a token, a score of -inf a beam (the first step has one live
+ * beam): such continuations come last, with score -inf.  NaN logits count as -inf, +inf as the largest finite number; a score
+ * that is not finite counts as -inf, and so do all of a beam without a logit above -inf.
+ * Supported: n_out <= 64, n_beams * vocab < 2^31. */
+size_t armt_beam_select_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out);
+armt_status armt_beam_select(const float *logits, int64_t ld_logits, const float *scores, int32_t n_seqs, int32_t n_beams, int32_t vocab,
+                             int32_t n_out, float *out_scores, int32_t *out_parents, int32_t *out_tokens,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The beams' states behind a selection: dst row (s, b) = src row (s, parents[s][b]) for every state, a row of row_bytes bytes per beam, rows
+ * src_stride / dst_stride bytes apart (0: dense): A [n_seqs * n_beams, L, d_model, Phi] and z of the batched forward calls, the
+ * pages of a beam, its tokens.  dst may be src (same stride); rows that continue themselves are then not touched.  Any other overlap of what is
+ * written is refused (ARMT_ERR_SHAPE).  parents [n_seqs, n_beams] are clamped into [0, n_beams).  At most 8 states, 64 beams. */
+typedef struct {
+  const void *src;
+  void *dst;
+  int64_t row_bytes, src_stride, dst_stride;
+} armt_beam_state;
+armt_status armt_beam_reorder(const int32_t *parents, int32_t n_seqs, int32_t n_beams, const armt_beam_state *states /* [host] */,
+                              int32_t n_states, void *hip_stream);
+
 /* Environment: ARMT_DEBUG_GENERIC=1 (read once per process) makes bf16 configurations run the plain
  * fp32-FMA GPU kernels of the fp32 path on bf16 operands instead of the MFMA kernels: slow, for telling an
  * error of a fast kernel from an error of the method.  Nothing ever runs on the host. */

@@ -15,10 +15,12 @@
 #include "attention_bwd_mfma.h"
 #include "attention_mfma.h"
 #include "backward_kernels.h"
+#include "beam.h"
 #include "common.h"
 #include "gemm_f32.h"
 #include "gemm_generic.h"
 #include "gemm_mfma.h"
+#include "kv_cache.h"
 #include "rowwise_kernels.h"
 #include "token_ends.h"
 
@@ -1059,3 +1061,4 @@ int32_t armt_timeline_read(unsigned long long* host, int64_t n_words) {
 }  // extern "C"
 
 #include "backward_host.h"
+#include "decode_host.h"

@@ -1,0 +1,716 @@
+// Keys and values of decoding: rows written into a paged cache with the rotation applied on the way, and the attention
+// of every sequence's new rows over its cached keys.
+//
+// A page holds page_len keys of every KV head, [Hkv][page_len][dh]; `pages` [n_seqs][max_pages] names the page of keys
+// j page_len .. of a sequence (an entry outside [0, n_pages) is no page: nothing is written there, and its keys do not exist).
+// Sequence s has lens[s] keys in front of this call's rows row_start[s] .. row_start[s + 1]; row i of them is key lens[s] + i.
+#pragma once
+
+#include <type_traits>
+
+#include "common.h"
+
+namespace armt {
+
+struct KvView {
+  const int32_t *pages, *lens, *row_start;
+  int n_seqs, n_pages, max_pages, page_shift, n_rows;
+  int64_t page_stride;      // elements from page to page
+};
+
+// ------------------------------------------------------------------------------------------------ append
+// q | k | v rows of the fused projection: q' = R(p) q -> q_out, k' = R(p) k and v -> the pages.  R(p) turns the pair
+// (j, j + dh/2) by p theta^(-2j/dh).  The angle is taken in turns and in double, and only its fraction is rounded to fp32: a position
+// of 10^6 loses nothing.  A block takes every gridDim.x-th row; its first dh/2 threads hold a frequency each and put a row's cos
+// and sin into LDS, all threads turn VEC pairs at a time.  Bytes bound it (each element read and written once).
+// grid: <= n_rows, block: 256.
+template <typename T, int VEC>
+struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
+
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qkv, int64_t ld, KvView c, const int32_t* __restrict__ positions,
+                                                        T* __restrict__ q_out, T* __restrict__ kc, T* __restrict__ vc,
+                                                        int H, int Hkv, int dh, double log2_theta) {
+  typedef Pack<T, VEC> V;
+  __shared__ float cs[2][128];           // [row parity][cos dh/2 | sin dh/2]
+  __shared__ int own[2];                 // sequence of the row (-1: nobody's)
+  const int half = dh >> 1, hv = half / VEC, rot_items = (H + Hkv) * hv, v_items = Hkv * (dh / VEC);
+  const int tid = threadIdx.x, P = 1 << c.page_shift;
+  double freq = 0.0;                     // turns per position
+  if (tid < half) freq = exp2(-(double)tid / (double)half * log2_theta) * 0.15915494309189533577;
+  int par = 0;
+  if (tid < 2) own[tid] = -1;
+  __syncthreads();
+  for (int64_t row = blockIdx.x; row < c.n_rows; row += gridDim.x, par ^= 1) {
+    for (int s = tid; s < c.n_seqs; s += blockDim.x)
+      if (row >= c.row_start[s] && row < c.row_start[s + 1]) own[par] = s;
+    __syncthreads();
+    const int s = own[par];
+    if (s < 0) { __syncthreads(); continue; }            // (uniform) behind the last sequence: left as it is
+    const int64_t slot = (int64_t)c.lens[s] + (row - c.row_start[s]);
+    if (tid < half) {
+      const double p = positions ? (double)positions[row] : (double)slot;
+      const double turn = p * freq;
+      const float f = 2.f * (float)(turn - rint(turn));
+      cs[par][tid] = cospif(f);
+      cs[par][half + tid] = sinpif(f);
+    }
+    __syncthreads();
+    if (tid == 0) own[par] = -1;                         // read again only behind the next row's barrier
+    bool live = slot >= 0 && (slot >> c.page_shift) < c.max_pages;
+    const int page = live ? c.pages[(int64_t)s * c.max_pages + (slot >> c.page_shift)] : -1;
+    live = live && page >= 0 && page < c.n_pages;
+    const int64_t at = (int64_t)(live ? page : 0) * c.page_stride + (slot & (P - 1)) * dh;
+    const T* src = qkv + row * ld;
+    for (int i = tid; i < rot_items + v_items; i += blockDim.x) {
+      if (i < rot_items) {
+        const int h = i / hv, j = (i - h * hv) * VEC;
+        const V a = *(const V*)(src + h * dh + j), b = *(const V*)(src + h * dh + half + j);
+        V x, y;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float co = cs[par][j + e], si = cs[par][half + j + e], u = to_f32(a.v[e]), w = to_f32(b.v[e]);
+          x.v[e] = from_f32<T>(u * co - w * si);
+          y.v[e] = from_f32<T>(w * co + u * si);
+        }
+        T* dst = h < H ? q_out + row * (int64_t)(H * dh) + h * dh : kc + at + (int64_t)(h - H) * P * dh;
+        if (h < H || live) {
+          *(V*)(dst + j) = x;
+          *(V*)(dst + half + j) = y;
+        }
+      } else if (live) {
+        const int h = (i - rot_items) / (dh / VEC), j = (i - rot_items - h * (dh / VEC)) * VEC;
+        *(V*)(vc + at + (int64_t)h * P * dh + j) = *(const V*)(src + (H + Hkv + h) * dh + j);
+      }
+    }
+  }
+}
+
+inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const KvView& c, const int32_t* positions, void* q_out,
+                                   void* k, void* v, int H, int Hkv, int dh, double theta, hipStream_t st) {
+  const unsigned grid = (unsigned)(c.n_rows < 2048 ? c.n_rows : 2048);       // eight blocks per compute unit
+  const double l2 = log2(theta);
+  if (bf)
+    kv_append_kernel<bf16, 8><<<grid, 256, 0, st>>>((const bf16*)qkv, ld, c, positions, (bf16*)q_out, (bf16*)k, (bf16*)v, H, Hkv, dh, l2);
+  else if (dh % 8 == 0)
+    kv_append_kernel<float, 4><<<grid, 256, 0, st>>>((const float*)qkv, ld, c, positions, (float*)q_out, (float*)k, (float*)v, H, Hkv, dh, l2);
+  else
+    kv_append_kernel<float, 2><<<grid, 256, 0, st>>>((const float*)qkv, ld, c, positions, (float*)q_out, (float*)k, (float*)v, H, Hkv, dh, l2);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+// out = softmax over the visible keys of (q . k / sqrt(dh)), times v, for the rows of every sequence and every head.
+// Row i of a sequence sees its context (keys < lens[s]) and, of the call's own keys, those of its mask bits (a tree of drafted
+// tokens) or those up to itself (no mask).  The rows of a KV head's query heads stand side by side: qi = i GROUP + g.
+//
+// A workgroup takes one slot (a run of keys of one sequence), one KV head and one block of 16 QT query rows; its four waves
+// take 32-key tiles in turn, every wave with a ring of tiles in LDS of its own that direct copies fill, so there is no barrier
+// among them until their results are joined.  Per tile a wave forms S^T = K Q^T (keys along the rows: a lane holds eight scores of ONE
+// query row, so the softmax needs no exchange until a reference has to move), P^T stays in the registers in which the second
+// product wants it, and V, which that product wants with the keys side by side, is read from its rows by transposing LDS reads.
+// Reading every key and value once bounds it for up to about 64 query rows.
+constexpr int KA_WAVES = 4;
+constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
+
+struct KvSeq { int s, len, row0, rows, total, first, last, count, slot0; };   // keys of a slot: [first, last)
+
+// The sequence and keys of slot w.  Every sequence has ceil(steps / per) slots, at least one, where a step is `step` keys and `per` the
+// least number for which all slots fit in n_seqs + spare.  All lanes of a wave work it out together, 64 sequences at a time.
+__device__ __forceinline__ void kv_extent(const KvView& c, int max_rows, int s, int& len, int& row0, int& rows, int& total) {
+  len = min(max(c.lens[s], 0), 1 << 30);
+  const int a = min(max(c.row_start[s], 0), c.n_rows), b = min(max(c.row_start[s + 1], a), c.n_rows);
+  row0 = a;
+  rows = min(b - a, max_rows);
+  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
+  total = (int)min((int64_t)len + rows, min(cap, (int64_t)0x7fffff00));
+}
+
+__device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int w, int spare, int step, KvSeq& q) {
+  const int lane = threadIdx.x & 63;
+  int len, row0, rows, total, per = 0x7fffffff;
+  q.s = -1;
+  if (spare == 0) {                        // one slot per sequence
+    if (w >= c.n_seqs) return false;
+    q.s = w; q.slot0 = w; q.count = 1;
+  } else {
+    int64_t sum = 0;
+    for (int b = 0; b < c.n_seqs; b += 64) {
+      int n = 0;
+      if (b + lane < c.n_seqs) {
+        kv_extent(c, max_rows, b + lane, len, row0, rows, total);
+        n = rows > 0 ? (total + step - 1) / step : 0;
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
+      sum += n;
+    }
+    per = (int)max((int64_t)1, (sum + spare - 1) / spare);
+    int before = 0;
+    for (int b = 0; b < c.n_seqs; b += 64) {
+      int n = 0;
+      if (b + lane < c.n_seqs) {
+        kv_extent(c, max_rows, b + lane, len, row0, rows, total);
+        n = max(1, rows > 0 ? ((total + step - 1) / step + per - 1) / per : 1);
+      }
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto, o, kWave);
+        if (lane >= o) upto += v;
+      }
+      const int start = before + upto - n;
+      const unsigned long long hit = __ballot(n > 0 && w >= start && w < start + n);
+      if (hit) {
+        const int l = __ffsll(hit) - 1;
+        q.s = b + l;
+        q.slot0 = __shfl(start, l, kWave);
+        q.count = __shfl(n, l, kWave);
+        break;
+      }
+      before += __shfl(upto, 63, kWave);
+    }
+    if (q.s < 0) return false;
+  }
+  q.s = __builtin_amdgcn_readfirstlane(q.s);
+  q.slot0 = __builtin_amdgcn_readfirstlane(q.slot0);
+  q.count = __builtin_amdgcn_readfirstlane(q.count);
+  kv_extent(c, max_rows, q.s, len, row0, rows, total);
+  q.len = __builtin_amdgcn_readfirstlane(len);
+  q.row0 = __builtin_amdgcn_readfirstlane(row0);
+  q.rows = __builtin_amdgcn_readfirstlane(rows);
+  q.total = __builtin_amdgcn_readfirstlane(total);
+  const int64_t first = q.count == 1 ? 0 : (int64_t)(w - q.slot0) * per * step;
+  q.first = __builtin_amdgcn_readfirstlane((int)min(first, (int64_t)q.total));
+  q.last = __builtin_amdgcn_readfirstlane(q.count == 1 ? q.total : (int)min(first + (int64_t)per * step, (int64_t)q.total));
+  return true;
+}
+
+// Geometry of a tile in LDS.  bf16: 32 keys, rows of DH x 2 bytes; fp32: 16 keys, rows of DH x 4 bytes (DH: dh rounded up to 32, 64 or
+// 128).  16-byte chunks of a row are exchanged (XOR) so that the reads of both products meet no bank twice: K is read
+// 16 rows at one chunk, V 8 rows at a pair of chunks (bf16) or whole rows (fp32).
+template <typename T, int DH>
+struct KvTile {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int KEYS = BF ? 32 : 16;
+  static constexpr int ROWB = DH * (int)sizeof(T);
+  static constexpr int BYTES = KEYS * ROWB;           // K or V
+  static constexpr int COPIES = BYTES / 1024;         // wave-wide copies of K or V
+  static constexpr int RPC = 1024 / ROWB;             // rows per copy
+  static constexpr int CHUNKS = ROWB / 16;
+  __device__ static __forceinline__ int swz_k(int row) { return ROWB == 128 ? (row >> 1) & 7 : row & 15; }
+  __device__ static __forceinline__ int swz_v(int row) { return !BF ? 0 : ROWB == 128 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; }
+};
+
+// A sequence's page table, read by scalar loads: the compiler's wait for a vector load would also wait for every copy in flight.
+typedef const __attribute__((address_space(4))) int32_t* kv_table_t;
+
+// Page bookkeeping of a wave's tile: base offsets (elements) of its 16-key halves, and which keys exist.
+template <typename T, int DH>
+struct KvHalves {
+  static constexpr int N = KvTile<T, DH>::KEYS / 16;
+  int64_t off[N];
+  unsigned have;      // bit h: half h lies on a page
+};
+
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+
+template <typename T, int DH>
+__device__ __forceinline__ KvHalves<T, DH> kv_halves(const KvView& c, kv_table_t table, int key0, int total, int kvh, int dh) {
+  KvHalves<T, DH> r;
+  r.have = 0;
+#pragma unroll
+  for (int h = 0; h < KvHalves<T, DH>::N; ++h) {
+    const int key = key0 + 16 * h;
+    const int j = min(key >> c.page_shift, c.max_pages - 1);
+    const int page = __builtin_amdgcn_readfirstlane(table[j]);
+    const bool ok = key < total && page >= 0 && page < c.n_pages;
+    r.have |= ok ? 1u << h : 0u;
+    r.off[h] = uniform64((int64_t)(ok ? page : 0) * c.page_stride + (int64_t)((kvh << c.page_shift) + (key & ((1 << c.page_shift) - 1))) * dh);
+  }
+  return r;
+}
+
+// Keys of a tile (bit x: key0 + x) below a limit.
+__device__ __forceinline__ unsigned keys_below(int limit, int key0) {
+  const int n = limit - key0;
+  return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
+}
+
+// What a query row sees: without a tree the keys below `limit`, with one those in front (uniform: len) and the drafts of its bits.
+struct KvMask { unsigned long long bits; int limit; };
+
+__device__ __forceinline__ unsigned keys_seen(const KvMask& m, bool tree, int len, int key0) {
+  if (!tree) return keys_below(m.limit, key0);
+  const int d = len - key0;          // drafts start at bit d
+  return keys_below(len, key0) | (d >= 32 ? 0u : d >= 0 ? (unsigned)(m.bits << d) : d > -64 ? (unsigned)(m.bits >> -d) : 0u);
+}
+
+template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// Max over the four lanes of a query row (lanes 16 apart).
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, kWave));
+  return fmaxf(v, __shfl_xor(v, 32, kWave));
+}
+
+// q, out: [n_rows][H dh]; tree: [n_rows] or null; part: [slots][Hkv][row blocks x 16 QT][DH] and pml: the same rows x {reference in log2,
+// sum} for sequences of more than one slot, whose {first slot, count} go to slot_of [n_seqs][2].
+// grid: 8 ceil(slots Hkv / 8) blocks; workgroup b belongs to XCD b % 8, and the row blocks that read the same keys stay on one
+// XCD, one behind the other.
+template <typename T, int DH, int QT, int S>
+__global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
+                                                                     const unsigned long long* __restrict__ tree, KvView c,
+                                                                     T* __restrict__ out, float* __restrict__ part, float* __restrict__ pml,
+                                                                     int32_t* __restrict__ slot_of, int H, int Hkv, int dh, int max_rows,
+                                                                     int slots, int spare, int blocks, float scale_log2e) {
+  typedef KvTile<T, DH> L;
+  constexpr bool BF = L::BF;
+  constexpr int KEYS = L::KEYS, ROWS = 16 * QT, NT = DH < 64 ? 4 : DH / 16, KS = BF ? DH / 32 : DH / 16, NS = KEYS / 4 / 4;
+  constexpr int STAGE = 2 * L::BYTES, NCOPY = 2 * L::COPIES;
+  extern __shared__ __align__(16) unsigned char smem[];      // [waves][S][STAGE]; then [waves][ROWS][DH] fp32 and [waves][ROWS][2]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int xj = blockIdx.x >> 3, rb = xj % blocks, pair = (xj / blocks) * 8 + (blockIdx.x & 7);
+  if (pair >= slots * Hkv) return;
+  const int w = pair / Hkv, kvh = pair - w * Hkv, group = H / Hkv;
+  KvSeq sq;
+  if (!kv_find_slot(c, max_rows, w, spare, KA_WAVES * KEYS, sq)) return;
+  if (spare && kvh == 0 && rb == 0 && threadIdx.x == 0 && w == sq.slot0) { slot_of[2 * sq.s] = w; slot_of[2 * sq.s + 1] = sq.count; }
+  const int q0 = rb * ROWS, nq = sq.rows * group;
+  if (q0 >= nq) return;
+
+  const int col = lane & 15, kg = lane >> 4;
+  // ---- query rows: B operand, lane = row col, 16 bytes at chunk 4 ks + kg
+  typedef typename std::conditional<BF, bf16x8, f32x4>::type frag_t;
+  frag_t qf[QT][KS];
+  KvMask mask[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int qi = q0 + t * 16 + col, i = qi / group, g = qi - i * group;
+    const bool live = qi < nq;
+    const int64_t row = sq.row0 + (live ? i : 0);
+    const T* p = q + row * (int64_t)(H * dh) + (kvh * group + g) * dh;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = (ks * 4 + kg) * (16 / (int)sizeof(T));
+#pragma unroll
+      for (int e = 0; e < 16 / (int)sizeof(T); ++e) qf[t][ks][e] = (T)0.f;
+      if (live && d < dh) qf[t][ks] = *(const frag_t*)(p + d);
+    }
+    mask[t].bits = live && tree ? tree[row] : ~0ull;         // rows of padding see everything: they must not look empty
+    mask[t].limit = live ? sq.len + i + 1 : 0x7fffffff;
+  }
+  // keys past the last row of the block are of no use without a tree
+  int last = sq.last;
+  if (!tree) last = __builtin_amdgcn_readfirstlane((int)min((int64_t)last, (int64_t)sq.len + (min(q0 + ROWS, nq) - 1) / group + 1));
+  const kv_table_t table = (kv_table_t)(uintptr_t)(c.pages + (int64_t)sq.s * c.max_pages);
+
+  // ---- copies: lane -> 16 bytes of row lane / CHUNKS of a copy's RPC rows
+  const int crow = lane / L::CHUNKS, cchunk = lane % L::CHUNKS;
+  const unsigned char* ring = smem + wave * (S * STAGE);
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) const void*)ring;
+  constexpr int PER = L::COPIES / KvHalves<T, DH>::N;       // copies of K, and of V, per 16-key half
+  unsigned vk[PER], vv[PER];                                // a lane's offsets from the half's base; the swizzles repeat every 16 rows
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int row = x * L::RPC + crow;
+    int ck = cchunk ^ L::swz_k(row), cv = cchunk ^ L::swz_v(row);
+    if (!BF && ck * 16 >= dh * 4) ck = 0;                   // padding of a short row: anything inside it
+    if (!BF && cv * 16 >= dh * 4) cv = 0;
+    vk[x] = (unsigned)(row * dh * (int)sizeof(T) + ck * 16);
+    vv[x] = (unsigned)(row * dh * (int)sizeof(T) + cv * 16);
+  }
+  auto issue = [&](const KvHalves<T, DH>& hv, int stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < L::COPIES; ++x) {
+      const int64_t off = hv.off[x / PER] * (int)sizeof(T);
+      lds_copy16((const char*)kc + off, vk[x % PER], lds0 + stage * STAGE + x * 1024);
+      lds_copy16((const char*)vc + off, vv[x % PER], lds0 + stage * STAGE + L::BYTES + x * 1024);
+    }
+  };
+
+  f32x4 o[QT][NT];
+  float m2[QT], lsum[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m2[t] = -INFINITY;
+    lsum[t] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int key_first = sq.first + wave * KEYS, stride = KA_WAVES * KEYS;
+  const int n = last > key_first ? (last - key_first + stride - 1) / stride : 0;
+  unsigned have[S];
+#pragma unroll
+  for (int x = 0; x < S - 1; ++x)
+    if (x < n) {
+      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, table, key_first + x * stride, sq.total, kvh, dh);
+      have[x] = hv.have;
+      issue(hv, x);
+    }
+
+  auto tile = [&](int it, int stage, unsigned pages_ok) __attribute__((always_inline)) {
+    unsigned char* Kt = (unsigned char*)ring + stage * STAGE;
+    unsigned char* Vt = Kt + L::BYTES;
+    const int key0 = key_first + it * stride;
+    const bool edge = key0 + KEYS > min(sq.len, last) || pages_ok != (1u << KvHalves<T, DH>::N) - 1;       // (uniform) some key is not everybody's
+    const unsigned exist = keys_below(sq.total, key0) & ((pages_ok & 1 ? 0xffffu : 0u) | (pages_ok & 2 ? 0xffff0000u : 0u));
+    unsigned bad = 0;       // keys whose values are not finite and not everybody's
+    if (edge) {
+      // Values that nobody sees become zero, since 0 x NaN is not; of the call's own keys, which some rows see, those with a value that
+      // is not finite are taken out of the product and added row by row below.
+#pragma unroll
+      for (int x = 0; x < L::COPIES; ++x) {
+        const int row = x * L::RPC + crow, key = key0 + row;
+        const bool none = !((exist >> row) & 1);
+        uint4* at = (uint4*)(Vt + x * 1024 + lane * 16);
+        const uint4 v = *at;
+        bool odd = false;
+        if (key >= sq.len && !none) {
+          const unsigned u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            odd |= BF ? (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u : (u[e] & 0x7f800000u) == 0x7f800000u;
+        }
+        unsigned long long odd_lanes = __ballot(odd);
+        while (odd_lanes) {
+          const int r = (__ffsll(odd_lanes) - 1) / L::CHUNKS;
+          bad |= 1u << (x * L::RPC + r);
+          odd_lanes &= ~(((1ull << L::CHUNKS) - 1) << (r * L::CHUNKS));
+        }
+        if (none || ((bad >> row) & 1)) *at = make_uint4(0, 0, 0, 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    // ---- fragments: K rows (A operand, lane = key row col), V transposed (A operand, lane = dimension)
+    frag_t kf[NS][KS], vf[BF ? NT : 4 * ((NT + 3) / 4)];
+#pragma unroll
+    for (int a = 0; a < NS; ++a)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int row = a * 16 + col;
+        kf[a][ks] = *(const frag_t*)(Kt + row * L::ROWB + (((ks * 4 + kg) ^ L::swz_k(row)) << 4));
+        if constexpr (!BF) {
+          if ((ks * 4 + kg) * 4 >= dh) kf[a][ks] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+    if constexpr (BF) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+      for (int d = 0; d < NT; ++d) {
+        s16x4 part4[2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          const int row = a * 16 + kg * 4 + (col >> 2), chunk = 2 * d + ((col & 3) >> 1);
+          part4[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(Vt + row * L::ROWB + ((chunk ^ L::swz_v(row)) << 4) + (col & 1) * 8));
+        }
+        vf[d] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(part4[0], part4[1], 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < (NT + 3) / 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int chunk = b * 16 + (DH < 64 ? min(col, L::CHUNKS - 1) : col);
+          vf[b * 4 + r] = *(const f32x4*)(Vt + (kg * 4 + r) * L::ROWB + chunk * 16);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      f32x4 sc[NS];
+#pragma unroll
+      for (int a = 0; a < NS; ++a) {
+        sc[a] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (BF) sc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[a][ks], qf[t][ks], sc[a], 0, 0, 0);
+          else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[a][ks][e], qf[t][ks][e], sc[a], 0, 0, 0);
+          }
+        }
+      }
+      unsigned seen = ~0u;
+      if (edge) {
+        seen = keys_seen(mask[t], tree != nullptr, sq.len, key0);
+        const unsigned mine = (seen & exist) >> (kg * 4);
+#pragma unroll
+        for (int a = 0; a < NS; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[a][r] = (mine >> (a * 16 + r)) & 1 ? sc[a][r] : -INFINITY;
+      }
+      // online softmax against a reference m2 (in log2 units) that moves only when a lane's probabilities of a tile add up to more than
+      // KA_LAZY_SUM or to nothing sensible (the first tile: exp2(s + inf))
+      float pr[NS][4], hs;
+      auto form = [&](float ref) __attribute__((always_inline)) {
+        hs = 0.f;
+#pragma unroll
+        for (int a = 0; a < NS; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            pr[a][r] = __builtin_amdgcn_exp2f(fmaf(sc[a][r], scale_log2e, -ref));
+            hs += pr[a][r];
+          }
+      };
+      form(m2[t]);
+      if (__builtin_amdgcn_ballot_w64(!(hs <= KA_LAZY_SUM)) != 0) {
+        float mx = sc[0][0];
+#pragma unroll
+        for (int a = 0; a < NS; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[a][r]);
+        const float m_new = fmaxf(m2[t], row_max(mx) * scale_log2e), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m2[t] - ref);      // 0 for a row that has seen nothing yet
+        m2[t] = m_new;
+        lsum[t] *= alpha;
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[t][d][r] *= alpha;
+        form(ref);
+      }
+      lsum[t] += hs;
+      if constexpr (BF) {
+        bf16x8 pf;
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) pf[a * 4 + r] = (bf16)pr[a][r];      // P in bf16: 2^-9 relative, as the operand of the matrix product
+#pragma unroll
+        for (int d = 0; d < NT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[(d / 4) * 4 + r][d % 4], pr[0][r], o[t][d], 0, 0, 0);
+      }
+      if (bad) {
+#pragma unroll
+        for (int a = 0; a < NS; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            for (int g = 0; g < 4; ++g) {
+              const int row = a * 16 + g * 4 + r;
+              if (!((bad >> row) & 1)) continue;
+              const int key = key0 + row;
+              const float p = __shfl(pr[a][r], g * 16 + col, kWave);
+              if (!((seen >> row) & 1)) continue;
+              const T* v = vc + (int64_t)table[key >> c.page_shift] * c.page_stride +
+                           (int64_t)((kvh << c.page_shift) + (key & ((1 << c.page_shift) - 1))) * dh;
+#pragma unroll
+              for (int d = 0; d < NT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int dim = BF ? d * 16 + kg * 4 + e : (d / 4) * 64 + kg * 16 + e * 4 + d % 4;
+                  if (dim < dh) o[t][d][e] = fmaf(p, to_f32(v[dim]), o[t][d][e]);
+                }
+            }
+      }
+    }
+  };
+
+  __builtin_amdgcn_s_waitcnt(0x0F70);       // query rows and first tiles: no wait of the compiler's is left for the loop
+  // ---- the wave's tiles: S - 1 of them in flight while one is worked on
+  int stage = 0;
+  KvHalves<T, DH> nx;
+  if (S - 1 < n) nx = kv_halves<T, DH>(c, table, key_first + (S - 1) * stride, sq.total, kvh, dh);
+  for (int it = 0; it < n; ++it) {
+    if (it + S - 1 < n) {
+      int into = stage + S - 1;
+      into = into >= S ? into - S : into;
+      have[S - 1] = nx.have;
+      issue(nx, into);
+      if (it + S < n) nx = kv_halves<T, DH>(c, table, key_first + (it + S) * stride, sq.total, kvh, dh);
+      wait_copies<(S - 1) * NCOPY>();
+    } else if (S > 2 && it + S - 2 < n) {
+      wait_copies<(S > 2 ? S - 2 : 0) * NCOPY>();
+    } else {
+      wait_copies<0>();
+    }
+    tile(it, stage, have[0]);
+#pragma unroll
+    for (int x = 0; x + 1 < S; ++x) have[x] = have[x + 1];
+    stage = stage + 1 == S ? 0 : stage + 1;
+  }
+
+  // ---- join the waves: rows of O (fp32) and {reference, sum} in LDS
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    lsum[t] += __shfl_xor(lsum[t], 16, kWave);
+    lsum[t] += __shfl_xor(lsum[t], 32, kWave);
+  }
+  __syncthreads();
+  float* Os = (float*)smem;
+  float* ML = Os + KA_WAVES * ROWS * DH;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float* r = Os + (size_t)(wave * ROWS + t * 16 + col) * DH;
+    if constexpr (BF) {
+#pragma unroll
+      for (int d = 0; d < NT; ++d) *(f32x4*)(r + d * 16 + kg * 4) = o[t][d];
+    } else {
+#pragma unroll
+      for (int b = 0; b < (NT + 3) / 4; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int dim = b * 64 + kg * 16 + e * 4;
+          if (dim < DH) *(f32x4*)(r + dim) = f32x4{o[t][b * 4][e], o[t][b * 4 + 1][e], o[t][b * 4 + 2][e], o[t][b * 4 + 3][e]};
+        }
+    }
+    if (kg == 0) { ML[(wave * ROWS + t * 16 + col) * 2] = m2[t]; ML[(wave * ROWS + t * 16 + col) * 2 + 1] = lsum[t]; }
+  }
+  __syncthreads();
+  const bool whole = sq.count == 1;
+  for (int x = threadIdx.x; x < ROWS * (DH / 4); x += KA_WAVES * 64) {
+    const int r = x / (DH / 4), d = (x - r * (DH / 4)) * 4, qi = q0 + r;
+    if (qi >= nq || d >= dh) continue;
+    float ref = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < KA_WAVES; ++v) ref = fmaxf(ref, ML[(v * ROWS + r) * 2]);
+    float sum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < KA_WAVES; ++v) {
+      const float mv = ML[(v * ROWS + r) * 2], f = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - ref);
+      const f32x4 ov = *(const f32x4*)(Os + (size_t)(v * ROWS + r) * DH + d);
+      if (mv == -INFINITY) continue;       // a wave without a visible key
+      sum = fmaf(f, ML[(v * ROWS + r) * 2 + 1], sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, ov[e], acc[e]);
+    }
+    if (whole) {
+      const float inv = ref == -INFINITY ? 0.f : 1.f / sum;       // a row that sees nothing is zero
+      const int i = qi / group, g = qi - i * group;
+      T* dst = out + (int64_t)(sq.row0 + i) * (H * dh) + (kvh * group + g) * dh + d;
+      Pack<T, 4> v4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v4.v[e] = from_f32<T>(ref == -INFINITY ? 0.f : acc[e] * inv);
+      *(Pack<T, 4>*)dst = v4;
+    } else {
+      const int64_t at = ((int64_t)w * Hkv + kvh) * (blocks * ROWS) + qi;
+      *(f32x4*)(part + at * DH + d) = acc;
+      if (d == 0) { pml[at * 2] = ref; pml[at * 2 + 1] = sum; }
+    }
+  }
+}
+
+// Rows of sequences that were cut into several slots: the slots' results joined.  grid: (n_rows, H), block: 64.
+template <typename T>
+__global__ __launch_bounds__(64) void kv_join_kernel(KvView c, T* __restrict__ out, const float* __restrict__ part, const float* __restrict__ pml,
+                                                     const int32_t* __restrict__ slot_of, int H, int Hkv, int dh, int DH, int max_rows,
+                                                     int prows) {
+  const int lane = threadIdx.x, h = blockIdx.y, group = H / Hkv, kvh = h / group;
+  const int64_t row = blockIdx.x;
+  int s = -1;
+  for (int b = 0; b < c.n_seqs && s < 0; b += 64) {
+    const bool mine = b + lane < c.n_seqs && row >= c.row_start[b + lane] && row < c.row_start[b + lane + 1];
+    const unsigned long long hit = __ballot(mine);
+    if (hit) s = b + __ffsll(hit) - 1;
+  }
+  if (s < 0) return;
+  const int i = (int)(row - max(c.row_start[s], 0));
+  const int slot = slot_of[2 * s], count = slot_of[2 * s + 1];
+  if (count <= 1 || i >= max_rows) return;
+  const int64_t at0 = ((int64_t)slot * Hkv + kvh) * prows + i * group + (h - kvh * group), step = (int64_t)Hkv * prows;
+  float ref = -INFINITY;
+  for (int n = lane; n < count; n += 64) ref = fmaxf(ref, pml[(at0 + n * step) * 2]);
+  ref = wave_max(ref);
+  float sum = 0.f, acc0 = 0.f, acc1 = 0.f;
+#pragma unroll 4
+  for (int n = 0; n < count; ++n) {
+    const int64_t at = at0 + n * step;
+    const float m = pml[at * 2], l = pml[at * 2 + 1];
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref);
+    const float a = lane < dh ? part[at * DH + lane] : 0.f, b = lane + 64 < dh ? part[at * DH + lane + 64] : 0.f;
+    if (m == -INFINITY) continue;
+    sum = fmaf(f, l, sum);
+    acc0 = fmaf(f, a, acc0);
+    acc1 = fmaf(f, b, acc1);
+  }
+  const float inv = ref == -INFINITY ? 0.f : 1.f / sum;
+  T* dst = out + row * (int64_t)(H * dh) + h * dh;
+  if (lane < dh) dst[lane] = from_f32<T>(ref == -INFINITY ? 0.f : acc0 * inv);
+  if (lane + 64 < dh) dst[lane + 64] = from_f32<T>(ref == -INFINITY ? 0.f : acc1 * inv);
+}
+
+// Shape of a launch, from what the host knows (the lengths are on the device).
+struct KvPlan {
+  int DH, QT, blocks, slots, spare;
+  size_t part, pml, slot_of, total;         // workspace
+};
+
+constexpr int KA_TARGET = 512;              // workgroups wanted: two per compute unit
+
+inline KvPlan kv_plan(bool bf, int n_seqs, int max_rows, int64_t max_keys, int H, int Hkv, int dh) {
+  KvPlan p;
+  p.DH = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
+  const int64_t nq = (int64_t)max_rows * (H / Hkv);
+  p.QT = nq <= 16 ? 1 : nq <= 32 || p.DH == 128 || !bf ? 2 : 4;
+  p.blocks = (int)((nq + 16 * p.QT - 1) / (16 * p.QT));
+  const int64_t step = KA_WAVES * (bf ? 32 : 16);
+  int64_t spare = KA_TARGET / ((int64_t)Hkv * p.blocks);
+  const int64_t most = n_seqs * ((max_keys + step - 1) / step - 1);       // cuts that keys could be made at
+  if (spare > most) spare = most;
+  p.spare = (int)(spare < 0 ? 0 : spare);
+  p.slots = n_seqs + p.spare;
+  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  const size_t rows = p.spare ? (size_t)p.slots * Hkv * p.blocks * 16 * p.QT : 0;
+  p.part = 0;
+  p.pml = up(rows * p.DH * 4);
+  p.slot_of = p.pml + up(rows * 8);
+  p.total = p.slot_of + (p.spare ? up((size_t)n_seqs * 8) : 0);
+  return p;
+}
+
+template <typename T, int DH, int QT, int S>
+hipError_t launch_kv_attention_as(const KvPlan& p, const void* q, const void* k, const void* v, const unsigned long long* tree, const KvView& c,
+                                  void* out, char* ws, int H, int Hkv, int dh, int max_rows, hipStream_t st) {
+  typedef KvTile<T, DH> L;
+  constexpr int ring = KA_WAVES * S * 2 * L::BYTES, join = KA_WAVES * 16 * QT * (DH + 2) * 4, lds = ring > join ? ring : join;
+  static std::atomic<uint64_t> raised{0};
+  if (lds > 65536) {
+    const hipError_t e = raise_lds_limit((const void*)kv_attention_kernel<T, DH, QT, S>, lds, raised);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t grid = 8 * (((int64_t)p.slots * Hkv + 7) / 8) * p.blocks;
+  kv_attention_kernel<T, DH, QT, S><<<(unsigned)grid, KA_WAVES * 64, lds, st>>>(
+      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, (float*)(ws + p.part), (float*)(ws + p.pml), (int32_t*)(ws + p.slot_of), H,
+      Hkv, dh, max_rows, p.slots, p.spare, p.blocks, 1.4426950408889634f / sqrtf((float)dh));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.spare) return e;
+  kv_join_kernel<T><<<dim3((unsigned)c.n_rows, H), 64, 0, st>>>(c, (T*)out, (const float*)(ws + p.part), (const float*)(ws + p.pml),
+                                                              (const int32_t*)(ws + p.slot_of), H, Hkv, dh, DH, max_rows, p.blocks * 16 * QT);
+  return hipGetLastError();
+}
+
+inline hipError_t launch_kv_attention(bool bf, const KvPlan& p, const void* q, const void* k, const void* v, const unsigned long long* tree,
+                                      const KvView& c, void* out, char* ws, int H, int Hkv, int dh, int max_rows, hipStream_t st) {
+#define ARMT_KA(T, D, Q, S) return launch_kv_attention_as<T, D, Q, S>(p, q, k, v, tree, c, out, ws, H, Hkv, dh, max_rows, st)
+  if (bf) {
+    if (p.DH == 64) {
+      if (p.QT == 1) ARMT_KA(bf16, 64, 1, 2);
+      if (p.QT == 2) ARMT_KA(bf16, 64, 2, 2);
+      ARMT_KA(bf16, 64, 4, 2);
+    }
+    if (p.QT == 1) ARMT_KA(bf16, 128, 1, 2);
+    ARMT_KA(bf16, 128, 2, 2);
+  }
+  if (p.DH == 32) {
+    if (p.QT == 1) ARMT_KA(float, 32, 1, 2);
+    ARMT_KA(float, 32, 2, 2);
+  }
+  if (p.DH == 64) {
+    if (p.QT == 1) ARMT_KA(float, 64, 1, 2);
+    ARMT_KA(float, 64, 2, 2);
+  }
+  if (p.QT == 1) ARMT_KA(float, 128, 1, 2);
+  ARMT_KA(float, 128, 2, 2);
+#undef ARMT_KA
+}
+
+}  // namespace armt

@@ -1,0 +1,300 @@
+"""The paged cache against float64: rows appended with their rotation, and attention of tokens, chains and trees of drafts over it."""
+import pytest
+import torch
+
+from decode_reference import HALF_STEP, Problem, rotate
+
+pytestmark = pytest.mark.gpu
+
+
+def assert_close(got, want, tol, what=""):
+    err = (got.double().cpu() - want).abs()
+    bad = ~(err <= tol)
+    assert not bad.any(), (what, int(bad.sum()), float((err / tol.clamp(min=1e-30))[bad].max()), bad.nonzero()[:4].tolist())
+
+
+# ------------------------------------------------------------------------------------------------ append
+APPEND = [
+    ("1b", "bf16", 64, [1040], [1]),
+    ("1b", "bf16", 16, [0, 5, 16, 1000], [1, 1, 20, 3]),
+    ("3b", "bf16", 128, [127, 128, 129], [2, 1, 130]),
+    ("160m", "bf16", 32, [3] * 70, [1] * 70),
+    ("tiny", "f32", 16, [0, 33, 7], [9, 0, 17]),
+    ("narrow", "f32", 16, [3, 15], [5, 2]),
+    ("wide", "f32", 32, [1, 31], [3, 40]),
+    ("8b", "f32", 64, [63], [2]),
+]
+
+
+def run_append(pr, qkv, positions=None):
+    cache = pr.on_gpu()
+    q = torch.full((pr.n_rows, pr.H * pr.dh), 77.0, dtype=pr.dt, device="cuda")
+    cache.append(qkv, *pr.args, positions=positions, out=q)
+    torch.cuda.synchronize()
+    return q.cpu(), pr.kd.cpu(), pr.vd.cpu()
+
+
+def check_append(pr, qkv, positions, got, theta=500000.0):
+    q, k, v = got
+    n = int(pr.row_start[-1])
+    x = qkv.cpu()[:n].view(n, pr.H + 2 * pr.Hkv, pr.dh)
+    # one product rounded, one fused: 2 u (|a| + |b|); the angle 2^-25 of a turn, its cosine and sine 4 u: together under 12 u of |a| + |b|
+    rot = rotate(x[:, :pr.H + pr.Hkv], positions[:n], theta)
+    size = x[:, :pr.H + pr.Hkv].double().abs()
+    size = size + size.roll(pr.dh // 2, -1)
+    tol = HALF_STEP[pr.dt] * rot.abs() + 12 * 2.0 ** -24 * size * 1.01
+    assert_close(q[:n].view(n, pr.H, pr.dh), rot[:, :pr.H], tol[:, :pr.H], "q")
+    assert (q[n:] == 77.0).all()
+    want_k, want_v = pr.k.clone(), pr.v.clone()
+    for s, r in enumerate(pr.rows):
+        for i in range(r):
+            row, t = int(pr.row_start[s]) + i, pr.lens[s] + i
+            if t // pr.page >= pr.pages.shape[1] or not 0 <= int(pr.pages[s, t // pr.page]) < k.shape[0]:
+                continue
+            p = int(pr.pages[s, t // pr.page])
+            assert_close(k[p, :, t % pr.page], rot[row, pr.H:], tol[row, pr.H:], ("k", s, i))
+            want_k[p, :, t % pr.page] = k[p, :, t % pr.page]
+            want_v[p, :, t % pr.page] = x[row, pr.H + pr.Hkv:]
+    as_bits = lambda a: a.view(torch.int16 if a.dtype == torch.bfloat16 else torch.int32)  # noqa: E731
+    assert torch.equal(as_bits(k.contiguous()), as_bits(want_k.contiguous()))            # nothing else was written
+    assert torch.equal(as_bits(v.contiguous()), as_bits(want_v.contiguous()))
+
+
+@pytest.mark.parametrize("heads,dtype,page,lens,rows", APPEND)
+def test_append(heads, dtype, page, lens, rows):
+    pr = Problem(heads, dtype, page, lens, rows, seed=len(lens), spare_rows=3)
+    qkv = torch.randn(pr.n_rows, (pr.H + 2 * pr.Hkv) * pr.dh, generator=pr.gen).to(pr.dt).cuda()
+    positions = torch.cat([torch.arange(l, l + r) for l, r in zip(lens, rows)] + [torch.zeros(3, dtype=torch.long)])
+    got = run_append(pr, qkv)
+    check_append(pr, qkv, positions, got)
+    again = run_append(pr, qkv, positions.int().cuda())                                  # the same, said explicitly
+    assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_positions_strides_and_missing_pages(dtype):
+    """Far positions (of a tree: not the slots), rows further apart, pages of two layers side by side, pages that do not exist, a full table."""
+    pr = Problem("tiny" if dtype == "f32" else "1b", dtype, 16, [10, 20, 30], [9, 13, 25], pool_pages=2)
+    width = (pr.H + 2 * pr.Hkv) * pr.dh
+    wide = torch.randn(pr.n_rows, width + 32, generator=pr.gen).to(pr.dt).cuda()
+    positions = torch.randint(0, 2 ** 31 - 1, (pr.n_rows,), generator=pr.gen).int()
+    pr.pages[0, 1] = -1
+    pr.pages[1, 2] = pr.k.shape[0]
+    pr.pages = pr.pages[:, :3].contiguous()                                              # the third sequence needs a fourth page
+    got = run_append(pr, wide[:, :width], positions.cuda())
+    check_append(pr, wide[:, :width].contiguous(), positions, got)
+
+
+# ------------------------------------------------------------------------------------------------ attention
+ATTEND = [
+    # heads, dtype, page, keys in front, rows, tree
+    ("1b", "bf16", 64, [1040], [1], False),
+    ("1b", "bf16", 16, [0, 1, 15, 16, 17, 31, 32, 33, 127, 128, 129], [1] * 11, False),
+    ("1b", "bf16", 64, [0, 5, 700, 130], [4, 1, 0, 9], True),
+    ("1b", "bf16", 32, [100, 260], [64, 13], True),
+    ("1b", "bf16", 64, [33, 0], [70, 150], False),
+    ("160m", "bf16", 128, [300, 2, 129], [1, 17, 40], False),
+    ("one", "bf16", 16, [500, 64], [5, 9], True),
+    ("3b", "bf16", 32, [200, 31], [1, 1], False),
+    ("3b", "bf16", 64, [260, 3, 0], [23, 64, 2], True),
+    ("8b", "bf16", 256, [515], [3], False),
+    ("tiny", "f32", 16, [0, 1, 15, 16, 64, 65, 300], [1] * 7, False),
+    ("tiny", "f32", 16, [40, 0, 90], [7, 33, 12], True),
+    ("narrow", "f32", 32, [50, 7], [9, 2], True),
+    ("wide", "f32", 16, [37, 100], [2, 11], False),
+    ("1b", "f32", 64, [200], [5], True),
+    ("8b", "f32", 32, [70, 3], [1, 30], False),
+]
+
+
+@pytest.mark.parametrize("heads,dtype,page,lens,rows,tree", ATTEND)
+def test_attention(heads, dtype, page, lens, rows, tree):
+    pr = Problem(heads, dtype, page, lens, rows, seed=7, spare_rows=2)
+    pr.own_keys()
+    q = pr.queries()
+    words = pr.trees() if tree else None
+    want, tol = pr.attend(q, words)
+    cache = pr.on_gpu()
+    out = torch.full_like(q, 55.0).cuda()
+    n = int(pr.row_start[-1])
+    for max_rows in (max(rows), max(rows) + 3 if not tree else 64):
+        out.fill_(55.0)
+        cache.attend(q.cuda(), *pr.args, max_rows, tree=None if words is None else words.cuda(), out=out)
+        torch.cuda.synchronize()
+        assert_close(out[:n], want[:n], tol[:n], max_rows)
+        assert (out[n:] == 55.0).all()
+
+
+def test_attention_of_many_cut_sequences():
+    """Enough keys that sequences are cut, more sequences than a wave has lanes, lengths from nothing to thousands."""
+    lens = [0 if s % 7 == 3 else 37 * s % 300 for s in range(70)] + [3000, 5000]
+    pr = Problem("one", "bf16", 64, lens, [s % 3 for s in range(70)] + [2, 1])
+    pr.own_keys()
+    q = pr.queries()
+    want, tol = pr.attend(q)
+    out = pr.on_gpu().attend(q.cuda(), *pr.args, 2)
+    assert_close(out, want, tol)
+
+
+@pytest.mark.parametrize("heads,dtype", [("1b", "bf16"), ("3b", "bf16"), ("tiny", "f32"), ("narrow", "f32")])
+def test_masks_that_leave_nothing_and_values_that_are_not_finite(heads, dtype):
+    """Rows without any key are zero; NaN and infinities of keys that a row does not see do not reach it, those that it sees do."""
+    pr = Problem(heads, dtype, 16, [0, 21, 0, 40], [6, 6, 3, 40], seed=3)
+    pr.own_keys()
+    q = pr.queries()
+    words = pr.trees()
+    words[0] = 0                                            # sees nothing: no context, no draft
+    words[13] = 0
+    words[6] = 0                                            # sees its context only
+    words[14] = (1 << 7) | (1 << 2)                         # bits of drafts that do not exist, and the last one
+    for s, i, value in ((0, 2, float("nan")), (1, 1, float("inf")), (1, 4, float("nan")), (3, 20, float("-inf")), (3, 33, float("nan"))):
+        t = pr.lens[s] + i
+        p = int(pr.pages[s, t // 16])
+        pr.v[p, :, t % 16, 1::5] = value
+        if i % 2:
+            pr.k[p, :, t % 16, ::3] = float("nan")
+    words[pr.row_start[3]:] &= ~((1 << 33) | (1 << 20))     # the last tree's rows see neither, but for one each
+    words[int(pr.row_start[3]) + 30] |= 1 << 20
+    want, tol = pr.attend(q, words)
+    out = pr.on_gpu().attend(q.cuda(), *pr.args, 40, tree=words.cuda()).cpu()
+    assert (out[0] == 0).all() and (out[13] == 0).all()
+    finite = want.isfinite()
+    assert finite[6].all() and (~finite).any() and finite.double().mean() > 0.6
+    assert torch.equal(out.isfinite(), finite)
+    assert torch.equal(out.double()[want.isinf()], want[want.isinf()])
+    assert_close(out[finite], want[finite], tol[finite])
+
+
+def test_pages_that_do_not_exist_and_a_table_that_is_too_short():
+    pr = Problem("1b", "bf16", 16, [100, 50, 64, 10], [3, 2, 1, 1], seed=5)
+    pr.own_keys()
+    q = pr.queries()
+    pr.pages[0, 2], pr.pages[0, 5] = -1, pr.k.shape[0]
+    pr.pages[1, :] = -7                                     # no page at all: zero
+    pr.pages = pr.pages[:, :6].contiguous()                 # the first sequence's last keys and rows have no entry
+    want, tol = pr.attend(q)
+    out = pr.on_gpu().attend(q.cuda(), *pr.args, 3).cpu()
+    assert (out[3:5] == 0).all()
+    assert_close(out, want, tol)
+
+
+def test_fewer_rows_than_a_sequence_has():
+    pr = Problem("tiny", "f32", 16, [20, 30], [5, 2])
+    pr.own_keys()
+    q = pr.queries()
+    out = torch.full_like(q, 9.0).cuda()
+    pr.on_gpu().attend(q.cuda(), *pr.args, 2, out=out)
+    want, tol = pr.attend(q, max_rows=2)
+    for r in (0, 1, 5, 6):
+        assert_close(out[r], want[r], tol[r], r)
+    assert (out[2:5] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_over_a_wide_range(dtype):
+    """Rising, falling and far scores: the reference of the softmax has to move, and must not lose what is small."""
+    pr = Problem("one" if dtype == "bf16" else "tiny", dtype, 16, [1500, 1500, 1500], [1, 1, 1], seed=11)
+    pr.own_keys()
+    q = pr.queries(std=1.0)
+    step = torch.arange(1500, dtype=torch.float64)
+    for s, scale in enumerate((step / 60, (1500 - step) / 60, torch.where(step == 700, 300.0, -40.0))):
+        direction = q[s].double().view(pr.H, pr.dh)[::pr.H // pr.Hkv]                   # along the first query head of every KV head
+        for t in range(1500):
+            k = direction / direction.norm(dim=-1, keepdim=True) * float(scale[t])
+            pr.k[int(pr.pages[s, t // 16]), :, t % 16] = k.to(pr.dt)
+    want, tol = pr.attend(q)
+    out = pr.on_gpu().attend(q.cuda(), *pr.args, 1)
+    assert_close(out, want, tol)
+
+
+def test_offsets_past_32_bits():
+    """Pages 2^29 elements apart: element offsets up to 2^32."""
+    pr = Problem("one", "bf16", 64, [300, 100], [2, 1], extra_pages=1)
+    pr.own_keys()
+    q = pr.queries()
+    want, tol = pr.attend(q)
+    cache_pages = pr.k.shape[0]
+    assert cache_pages <= 9
+    import paper_2506_05229_amd as P
+    far = []
+    for host in (pr.k, pr.v):
+        pool = torch.empty((cache_pages - 1) * 2 ** 29 + host[0].numel(), dtype=pr.dt, device="cuda")
+        view = pool.as_strided(tuple(host.shape), (2 ** 29,) + tuple(host[0].contiguous().stride()))
+        view.copy_(host)
+        far.append(view)
+    cache = P.KvCache(pr.shape, *far)
+    args = (pr.pages.cuda(), torch.tensor(pr.lens, dtype=torch.int32).cuda(), pr.row_start.cuda())
+    out = cache.attend(q.cuda(), *args, 2)
+    assert_close(out, want, tol)
+    qkv = torch.randn(pr.n_rows, (pr.H + 2 * pr.Hkv) * pr.dh, generator=pr.gen).to(pr.dt).cuda()
+    q_near = pr.on_gpu().append(qkv, *pr.args)
+    q_far = cache.append(qkv, *args)
+    torch.cuda.synchronize()
+    bits = lambda a: a.contiguous().view(torch.int16)  # noqa: E731
+    assert torch.equal(q_near, q_far) and torch.equal(bits(pr.kd), bits(far[0])) and torch.equal(bits(pr.vd), bits(far[1]))
+
+
+def test_replay_from_a_graph_while_lengths_grow():
+    """One token per replay: append and attention recorded once; lengths, tables and rows change in place between the replays."""
+    pr = Problem("1b", "bf16", 16, [60, 13], [4, 4], seed=2)
+    cache = pr.on_gpu()
+    pages, lens, row_start = pr.args[0], torch.tensor([60, 13], dtype=torch.int32).cuda(), torch.tensor([0, 1, 2], dtype=torch.int32).cuda()
+    width = (pr.H + 2 * pr.Hkv) * pr.dh
+    rows = torch.randn(4, 2, width, generator=pr.gen).to(pr.dt).cuda()
+    qkv, out, q = rows[0].clone(), torch.empty(2, pr.H * pr.dh, dtype=pr.dt, device="cuda"), torch.empty(2, pr.H * pr.dh, dtype=pr.dt, device="cuda")
+
+    def step():
+        cache.append(qkv, pages, lens, row_start, out=q)
+        cache.attend(q, pages, lens, row_start, 1, out=out)
+
+    eager = []
+    for t in range(4):
+        qkv.copy_(rows[t])
+        step()
+        eager.append(out.clone())
+        lens += 1
+    torch.cuda.synchronize()
+    lens -= 4
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t in range(4):
+        qkv.copy_(rows[t])
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[t]), t
+        cache.attend(q, pages, lens, row_start, 1)           # eager work of the same kind in between
+        lens += 1
+
+
+def test_calls_on_two_streams():
+    a, b = (Problem("1b", "bf16", 64, [900 + 50 * i, 1500], [2, 1], seed=i) for i in range(2))
+    jobs = []
+    for pr in (a, b):
+        pr.own_keys()
+        jobs.append((pr, pr.on_gpu(), pr.queries().cuda(), torch.cuda.Stream()))
+    want = [c.attend(q, *pr.args, 2) for pr, c, q, _ in jobs]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(20):
+        for i, (pr, c, q, st) in enumerate(jobs):
+            with torch.cuda.stream(st):
+                outs[i].append(c.attend(q, *pr.args, 2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in outs[i])
+
+
+def test_chain_of_one_token_calls_equals_one_call():
+    """Tokens appended and attended one by one see what a chain of them in one call sees."""
+    pr = Problem("3b", "bf16", 32, [77], [6], seed=4)
+    qkv = torch.randn(6, (pr.H + 2 * pr.Hkv) * pr.dh, generator=pr.gen).to(pr.dt).cuda()
+    cache = pr.on_gpu()
+    whole = cache.attend(cache.append(qkv, *pr.args), *pr.args, 6)
+    cache = pr.on_gpu()
+    one = torch.tensor([0, 1], dtype=torch.int32).cuda()
+    for i in range(6):
+        lens = torch.tensor([77 + i], dtype=torch.int32).cuda()
+        got = cache.attend(cache.append(qkv[i:i + 1], pr.args[0], lens, one), pr.args[0], lens, one, 1)
+        # both are within half a step of the output and of each probability
+        assert_close(got[0], whole[i].double().cpu(), 2 * 2.0 ** -8 * (whole[i].double().cpu().abs() + 1.0), i)
