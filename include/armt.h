@@ -363,7 +363,8 @@ armt_status armt_kv_append(const armt_config *cfg, const armt_kv_cache *cache, c
  * rows of any sequence (a longer sequence's further rows are left as they are).  Scores, probabilities' sums and outputs are
  * accumulated in fp32; in bf16 the probabilities are rounded to bf16 for the second product.  The workspace is
  * armt_kv_attention_workspace_bytes (0 = rejected) and 256-byte aligned; calls that may overlap need one each. */
-size_t armt_kv_attention_workspace_bytes(const armt_config *cfg, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t max_rows);
+size_t armt_kv_attention_workspace_bytes(const armt_config *cfg, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t n_rows,
+                                         int32_t max_rows);
 armt_status armt_kv_attention(const armt_config *cfg, const armt_kv_cache *cache, const void *q, int32_t n_rows, int32_t max_rows,
                               const uint64_t *tree, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -133,7 +133,7 @@ def load_library():
     kv = C.POINTER(ArmtKvCache)
     lib.armt_kv_append.argtypes = [C.POINTER(ArmtConfig), kv, vp, i64, i32, vp, vp, vp]
     lib.armt_kv_append.restype = C.c_int
-    lib.armt_kv_attention_workspace_bytes.argtypes = [C.POINTER(ArmtConfig), i32, i32, i32, i32]
+    lib.armt_kv_attention_workspace_bytes.argtypes = [C.POINTER(ArmtConfig), i32, i32, i32, i32, i32]
     lib.armt_kv_attention_workspace_bytes.restype = sz
     lib.armt_kv_attention.argtypes = [C.POINTER(ArmtConfig), kv, vp, i32, i32, vp, vp, vp, sz, vp]
     lib.armt_kv_attention.restype = C.c_int
@@ -562,7 +562,7 @@ class KvCache:
         c = self._call(pages, lens, row_start)
         if tree is not None:
             assert tree.device == self.device and tree.dtype == torch.int64 and tree.shape == (n,) and tree.is_contiguous()
-        need = self.lib.armt_kv_attention_workspace_bytes(self._cfg_ref, c.n_seqs, c.max_pages, self.page_len, max_rows)
+        need = self.lib.armt_kv_attention_workspace_bytes(self._cfg_ref, c.n_seqs, c.max_pages, self.page_len, n, max_rows)
         if need == 0:
             raise ArmtError(2, "configuration or sizes rejected by armt_kv_attention_workspace_bytes")
         with _on(torch, self.device):

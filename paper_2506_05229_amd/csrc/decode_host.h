@@ -24,10 +24,10 @@ armt_status check_cache(const armt_config* cfg, const armt_kv_cache* cache, int3
 }
 
 // Grid and workspace limits of the attention; false: too large for a launch.
-bool attention_plan(const Dims& D, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t max_rows, KvPlan* p) {
+bool attention_plan(const Dims& D, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t n_rows, int32_t max_rows, KvPlan* p) {
   if ((int64_t)max_rows * (D.H / D.Hkv) > 1 << 30) return false;
-  *p = kv_plan(D.bf16, n_seqs, max_rows, (int64_t)max_pages * page_len, D.H, D.Hkv, D.dh);
-  return 8 * (((int64_t)p->slots * D.Hkv + 7) / 8) * p->blocks <= 0x7fffffff && D.H <= 65535;
+  *p = kv_plan(D.bf16, n_seqs, n_rows, max_rows, (int64_t)max_pages * page_len, D.H, D.Hkv, D.dh);
+  return 8 * (((int64_t)p->slots * D.Hkv + 7) / 8) * p->blocks <= 0x7fffffff && (int64_t)n_rows * D.H <= 0x7fffffff;
 }
 
 // Whether two sets of n rows may share memory (rows of equal stride may lie between each other).
@@ -55,11 +55,11 @@ armt_status armt_kv_append(const armt_config* cfg, const armt_kv_cache* cache, c
   return ARMT_OK;
 }
 
-size_t armt_kv_attention_workspace_bytes(const armt_config* cfg, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t max_rows) {
+size_t armt_kv_attention_workspace_bytes(const armt_config* cfg, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t n_rows, int32_t max_rows) {
   Dims D;
   KvPlan p;
-  if (check_config(cfg, &D) != ARMT_OK || n_seqs < 1 || n_seqs > kMaxSeqs || max_pages < 1 || page_len < 1 || max_rows < 1 ||
-      !attention_plan(D, n_seqs, max_pages, page_len, max_rows, &p))
+  if (check_config(cfg, &D) != ARMT_OK || n_seqs < 1 || n_seqs > kMaxSeqs || max_pages < 1 || page_len < 1 || n_rows < 1 || max_rows < 1 ||
+      !attention_plan(D, n_seqs, max_pages, page_len, n_rows, max_rows, &p))
     return 0;
   return p.total > kAlign ? p.total : kAlign;
 }
@@ -73,7 +73,7 @@ armt_status armt_kv_attention(const armt_config* cfg, const armt_kv_cache* cache
   if (!q || !out) return ARMT_ERR_NULL;
   if (max_rows < 1 || (tree && max_rows > 64)) return ARMT_ERR_SHAPE;
   if ((uintptr_t)q % 16 || (uintptr_t)out % 16) return ARMT_ERR_UNSUPPORTED;
-  if (!attention_plan(D, cache->n_seqs, cache->max_pages, cache->page_len, max_rows, &p)) return ARMT_ERR_UNSUPPORTED;
+  if (!attention_plan(D, cache->n_seqs, cache->max_pages, cache->page_len, n_rows, max_rows, &p)) return ARMT_ERR_UNSUPPORTED;
   if (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < std::max(p.total, kAlign)) return ARMT_ERR_WORKSPACE;
   HIP_TRY(launch_kv_attention(D.bf16, p, q, cache->k, cache->v, (const unsigned long long*)tree, v, out, (char*)workspace, D.H, D.Hkv, D.dh, max_rows,
                               (hipStream_t)hip_stream));

@@ -21,81 +21,101 @@ struct KvView {
 // ------------------------------------------------------------------------------------------------ append
 // q | k | v rows of the fused projection: q' = R(p) q -> q_out, k' = R(p) k and v -> the pages.  R(p) turns the pair
 // (j, j + dh/2) by p theta^(-2j/dh).  The angle is taken in turns and in double, and only its fraction is rounded to fp32: a position
-// of 10^6 loses nothing.  A block takes every gridDim.x-th row; its first dh/2 threads hold a frequency each and put a row's cos
-// and sin into LDS, all threads turn VEC pairs at a time.  Bytes bound it (each element read and written once).
-// grid: <= n_rows, block: 256.
+// of 10^9 loses nothing.  A block takes `per` rows: first where each of them goes and the cosines and sines of all of them, into LDS, then VEC pairs
+// at a time without another barrier; a thread's first loads are on their way before the first barrier.  Bytes bound it (each
+// element read and written once), for few rows the two loads that lead to a row's page.
+// grid: ceil(n_rows / per), block: 256.
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
+
+constexpr int KV_ROWS = 4;               // most rows of a block
 
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qkv, int64_t ld, KvView c, const int32_t* __restrict__ positions,
                                                         T* __restrict__ q_out, T* __restrict__ kc, T* __restrict__ vc,
-                                                        int H, int Hkv, int dh, double log2_theta) {
+                                                        int H, int Hkv, int dh, int per, double log2_theta) {
   typedef Pack<T, VEC> V;
-  __shared__ float cs[2][128];           // [row parity][cos dh/2 | sin dh/2]
-  __shared__ int own[2];                 // sequence of the row (-1: nobody's)
-  const int half = dh >> 1, hv = half / VEC, rot_items = (H + Hkv) * hv, v_items = Hkv * (dh / VEC);
+  __shared__ float cs[KV_ROWS][128];     // cos dh/2 | sin dh/2
+  __shared__ int64_t at[KV_ROWS];        // element of the key in head 0 of its page; -1: no page; -2: nobody's row
+  __shared__ int64_t slot[KV_ROWS];
+  const int half = dh >> 1, hv = half / VEC, rot_items = (H + Hkv) * hv, dv = dh / VEC, row_items = rot_items + Hkv * dv;
   const int tid = threadIdx.x, P = 1 << c.page_shift;
-  double freq = 0.0;                     // turns per position
-  if (tid < half) freq = exp2(-(double)tid / (double)half * log2_theta) * 0.15915494309189533577;
-  int par = 0;
-  if (tid < 2) own[tid] = -1;
+  const int64_t row0 = (int64_t)blockIdx.x * per;
+  const int rows = (int)min((int64_t)per, c.n_rows - row0), items = rows * row_items;
+  // item i: pair of VEC columns (j, j + half) of rotated head h, or VEC columns of a value head
+  auto place = [&](int i, int& r, int& h, int& j) __attribute__((always_inline)) {
+    r = i / row_items;
+    const int x = i - r * row_items;
+    if (x < rot_items) { h = x / hv; j = (x - h * hv) * VEC; }
+    else { h = (x - rot_items) / dv; j = (x - rot_items - h * dv) * VEC; h += H + Hkv; }
+  };
+  V a, b;
+  int r1 = 0, h1 = 0, j1 = 0;            // place of the item whose values are in a, b
+  auto load = [&](int i) __attribute__((always_inline)) {
+    place(i, r1, h1, j1);
+    const T* src = qkv + (row0 + r1) * ld + h1 * dh + j1;
+    a = *(const V*)src;
+    if (h1 < H + Hkv) b = *(const V*)(src + half);
+  };
+  if (tid < items) load(tid);
+  static_assert(KV_ROWS * 64 <= 256, "an angle per thread");
+  const int ar = tid / half, aj = tid - ar * half, pos = positions && ar < rows ? positions[row0 + ar] : 0;
+  if (tid < KV_ROWS) { at[tid] = -2; slot[tid] = 0; }
   __syncthreads();
-  for (int64_t row = blockIdx.x; row < c.n_rows; row += gridDim.x, par ^= 1) {
-    for (int s = tid; s < c.n_seqs; s += blockDim.x)
-      if (row >= c.row_start[s] && row < c.row_start[s + 1]) own[par] = s;
-    __syncthreads();
-    const int s = own[par];
-    if (s < 0) { __syncthreads(); continue; }            // (uniform) behind the last sequence: left as it is
-    const int64_t slot = (int64_t)c.lens[s] + (row - c.row_start[s]);
-    if (tid < half) {
-      const double p = positions ? (double)positions[row] : (double)slot;
-      const double turn = p * freq;
-      const float f = 2.f * (float)(turn - rint(turn));
-      cs[par][tid] = cospif(f);
-      cs[par][half + tid] = sinpif(f);
+  for (int s = tid; s < c.n_seqs; s += 256) {
+    const int64_t lo = c.row_start[s], hi = c.row_start[s + 1], len = c.lens[s];
+    for (int64_t r = max(lo, row0); r < min(hi, row0 + rows); ++r) {
+      const int64_t k = len + (r - lo), j = k >> c.page_shift;
+      const int page = k >= 0 && j < c.max_pages ? c.pages[(int64_t)s * c.max_pages + j] : -1;
+      slot[r - row0] = k;
+      at[r - row0] = page >= 0 && page < c.n_pages ? (int64_t)page * c.page_stride + (k & (P - 1)) * dh : -1;
     }
-    __syncthreads();
-    if (tid == 0) own[par] = -1;                         // read again only behind the next row's barrier
-    bool live = slot >= 0 && (slot >> c.page_shift) < c.max_pages;
-    const int page = live ? c.pages[(int64_t)s * c.max_pages + (slot >> c.page_shift)] : -1;
-    live = live && page >= 0 && page < c.n_pages;
-    const int64_t at = (int64_t)(live ? page : 0) * c.page_stride + (slot & (P - 1)) * dh;
-    const T* src = qkv + row * ld;
-    for (int i = tid; i < rot_items + v_items; i += blockDim.x) {
-      if (i < rot_items) {
-        const int h = i / hv, j = (i - h * hv) * VEC;
-        const V a = *(const V*)(src + h * dh + j), b = *(const V*)(src + h * dh + half + j);
-        V x, y;
+  }
+  if (!positions) __syncthreads();
+  if (ar < rows) {
+    const double turn = (positions ? (double)pos : (double)slot[ar]) * (exp2(-(double)aj / (double)half * log2_theta) * 0.15915494309189533577);
+    const float f = 2.f * (float)(turn - rint(turn));
+    cs[ar][aj] = cospif(f);
+    cs[ar][half + aj] = sinpif(f);
+  }
+  __syncthreads();
+  for (int i = tid; i < items;) {
+    const int r = r1, h = h1, j = j1;
+    const int64_t to = at[r];
+    const V a0 = a, b0 = b;
+    i += 256;
+    if (i < items) load(i);
+    if (to == -2) continue;              // behind the last sequence: left as it is
+    if (h < H + Hkv) {
+      V x, y;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float co = cs[par][j + e], si = cs[par][half + j + e], u = to_f32(a.v[e]), w = to_f32(b.v[e]);
-          x.v[e] = from_f32<T>(u * co - w * si);
-          y.v[e] = from_f32<T>(w * co + u * si);
-        }
-        T* dst = h < H ? q_out + row * (int64_t)(H * dh) + h * dh : kc + at + (int64_t)(h - H) * P * dh;
-        if (h < H || live) {
-          *(V*)(dst + j) = x;
-          *(V*)(dst + half + j) = y;
-        }
-      } else if (live) {
-        const int h = (i - rot_items) / (dh / VEC), j = (i - rot_items - h * (dh / VEC)) * VEC;
-        *(V*)(vc + at + (int64_t)h * P * dh + j) = *(const V*)(src + (H + Hkv + h) * dh + j);
+      for (int e = 0; e < VEC; ++e) {
+        const float co = cs[r][j + e], si = cs[r][half + j + e], u = to_f32(a0.v[e]), w = to_f32(b0.v[e]);
+        x.v[e] = from_f32<T>(u * co - w * si);
+        y.v[e] = from_f32<T>(w * co + u * si);
       }
+      T* dst = h < H ? q_out + (row0 + r) * (int64_t)(H * dh) + h * dh : kc + to + (int64_t)(h - H) * P * dh;
+      if (h < H || to >= 0) {
+        *(V*)(dst + j) = x;
+        *(V*)(dst + half + j) = y;
+      }
+    } else if (to >= 0) {
+      *(V*)(vc + to + (int64_t)(h - H - Hkv) * P * dh + j) = a0;
     }
   }
 }
 
 inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const KvView& c, const int32_t* positions, void* q_out,
                                    void* k, void* v, int H, int Hkv, int dh, double theta, hipStream_t st) {
-  const unsigned grid = (unsigned)(c.n_rows < 2048 ? c.n_rows : 2048);       // eight blocks per compute unit
+  int per = (c.n_rows + 2047) / 2048;                  // eight blocks per compute unit as long as a block takes no more than its rows
+  per = per > KV_ROWS ? KV_ROWS : per;
+  const unsigned grid = (unsigned)(((int64_t)c.n_rows + per - 1) / per);
   const double l2 = log2(theta);
-  if (bf)
-    kv_append_kernel<bf16, 8><<<grid, 256, 0, st>>>((const bf16*)qkv, ld, c, positions, (bf16*)q_out, (bf16*)k, (bf16*)v, H, Hkv, dh, l2);
-  else if (dh % 8 == 0)
-    kv_append_kernel<float, 4><<<grid, 256, 0, st>>>((const float*)qkv, ld, c, positions, (float*)q_out, (float*)k, (float*)v, H, Hkv, dh, l2);
-  else
-    kv_append_kernel<float, 2><<<grid, 256, 0, st>>>((const float*)qkv, ld, c, positions, (float*)q_out, (float*)k, (float*)v, H, Hkv, dh, l2);
+#define ARMT_KV(T, VEC) kv_append_kernel<T, VEC><<<grid, 256, 0, st>>>((const T*)qkv, ld, c, positions, (T*)q_out, (T*)k, (T*)v, H, Hkv, dh, per, l2)
+  if (bf) ARMT_KV(bf16, 8);
+  else if (dh % 8 == 0) ARMT_KV(float, 4);
+  else ARMT_KV(float, 2);
+#undef ARMT_KV
   return hipGetLastError();
 }
 
@@ -110,79 +130,87 @@ inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const K
 // query row, so the softmax needs no exchange until a reference has to move), P^T stays in the registers in which the second
 // product wants it, and V, which that product wants with the keys side by side, is read from its rows by transposing LDS reads.
 // Reading every key and value once bounds it for up to about 64 query rows.
-constexpr int KA_WAVES = 4;
+constexpr int KA_STEP = 128;              // keys are cut into slots at multiples of this
+constexpr int KA_TARGET = 512;            // workgroups wanted: two per compute unit
 constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
 
-struct KvSeq { int s, len, row0, rows, total, first, last, count, slot0; };   // keys of a slot: [first, last)
+struct KvSeq { int s, len, row0, rows, all, total, first, last, count, slot0; };   // keys of a slot: [first, last)
 
-// The sequence and keys of slot w.  Every sequence has ceil(steps / per) slots, at least one, where a step is `step` keys and `per` the
-// least number for which all slots fit in n_seqs + spare.  All lanes of a wave work it out together, 64 sequences at a time.
-__device__ __forceinline__ void kv_extent(const KvView& c, int max_rows, int s, int& len, int& row0, int& rows, int& total) {
-  len = min(max(c.lens[s], 0), 1 << 30);
-  const int a = min(max(c.row_start[s], 0), c.n_rows), b = min(max(c.row_start[s + 1], a), c.n_rows);
-  row0 = a;
-  rows = min(b - a, max_rows);
-  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
-  total = (int)min((int64_t)len + rows, min(cap, (int64_t)0x7fffff00));
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v) {
+#define ARMT_DPP(ctrl, rows) v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
+  ARMT_DPP(0x111, 0xf);      // row_shr:1, 2, 4, 8 inside rows of 16 lanes
+  ARMT_DPP(0x112, 0xf);
+  ARMT_DPP(0x114, 0xf);
+  ARMT_DPP(0x118, 0xf);
+  ARMT_DPP(0x142, 0xa);      // row_bcast:15, 31
+  ARMT_DPP(0x143, 0xc);
+#undef ARMT_DPP
+  return v;
 }
 
+// The sequence and keys of slot w.  A sequence of n steps (of `step` keys) has ceil(n / per) slots of equal length, at least one; `per` is the
+// least number for which all slots fit in n_seqs + spare.  All lanes of a wave work it out together, 64 sequences at a time.
 __device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int w, int spare, int step, KvSeq& q) {
   const int lane = threadIdx.x & 63;
-  int len, row0, rows, total, per = 0x7fffffff;
-  q.s = -1;
+  int len, row0, rows, all, total, steps;
+  auto load = [&](int s) __attribute__((always_inline)) {
+    const int64_t cap = (int64_t)c.max_pages << c.page_shift;
+    len = c.lens[s];
+    const int a = c.row_start[s], b = c.row_start[s + 1];
+    len = min(max(len, 0), 1 << 30);
+    row0 = min(max(a, 0), c.n_rows);
+    all = min(max(b, row0), c.n_rows) - row0;
+    rows = min(all, max_rows);
+    total = (int)min((int64_t)len + rows, cap);
+    steps = rows > 0 ? (total + step - 1) / step : 0;
+  };
+  int s = w, slot0 = w, count = 1;
   if (spare == 0) {                        // one slot per sequence
     if (w >= c.n_seqs) return false;
-    q.s = w; q.slot0 = w; q.count = 1;
+    load(w);
   } else {
     int64_t sum = 0;
     for (int b = 0; b < c.n_seqs; b += 64) {
-      int n = 0;
-      if (b + lane < c.n_seqs) {
-        kv_extent(c, max_rows, b + lane, len, row0, rows, total);
-        n = rows > 0 ? (total + step - 1) / step : 0;
-      }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
-      sum += n;
+      load(min(b + lane, c.n_seqs - 1));
+      sum += __builtin_amdgcn_readlane(wave_scan(b + lane < c.n_seqs ? steps : 0), 63);
     }
-    per = (int)max((int64_t)1, (sum + spare - 1) / spare);
+    const int per = sum > 0x7fff0000 - spare ? 0x7fffffff : max(1, ((int)sum + spare - 1) / spare);
     int before = 0;
+    s = -1;
     for (int b = 0; b < c.n_seqs; b += 64) {
-      int n = 0;
-      if (b + lane < c.n_seqs) {
-        kv_extent(c, max_rows, b + lane, len, row0, rows, total);
-        n = max(1, rows > 0 ? ((total + step - 1) / step + per - 1) / per : 1);
-      }
-      int upto = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += v;
-      }
-      const int start = before + upto - n;
-      const unsigned long long hit = __ballot(n > 0 && w >= start && w < start + n);
+      if (c.n_seqs > 64) load(min(b + lane, c.n_seqs - 1));
+      const int n = b + lane < c.n_seqs ? max(1, (int)(((int64_t)steps + per - 1) / per)) : 0;
+      const int upto = wave_scan(n), start = before + upto - n;
+      const unsigned long long hit = __ballot(w >= start && w < start + n);
       if (hit) {
         const int l = __ffsll(hit) - 1;
-        q.s = b + l;
-        q.slot0 = __shfl(start, l, kWave);
-        q.count = __shfl(n, l, kWave);
+        s = b + l;
+        slot0 = __builtin_amdgcn_readlane(start, l);
+        count = __builtin_amdgcn_readlane(n, l);
+        len = __builtin_amdgcn_readlane(len, l);
+        row0 = __builtin_amdgcn_readlane(row0, l);
+        rows = __builtin_amdgcn_readlane(rows, l);
+        all = __builtin_amdgcn_readlane(all, l);
+        total = __builtin_amdgcn_readlane(total, l);
+        steps = __builtin_amdgcn_readlane(steps, l);
         break;
       }
-      before += __shfl(upto, 63, kWave);
+      before += __builtin_amdgcn_readlane(upto, 63);
     }
-    if (q.s < 0) return false;
+    if (s < 0) return false;
   }
-  q.s = __builtin_amdgcn_readfirstlane(q.s);
-  q.slot0 = __builtin_amdgcn_readfirstlane(q.slot0);
-  q.count = __builtin_amdgcn_readfirstlane(q.count);
-  kv_extent(c, max_rows, q.s, len, row0, rows, total);
+  q.s = __builtin_amdgcn_readfirstlane(s);
+  q.slot0 = __builtin_amdgcn_readfirstlane(slot0);
+  q.count = __builtin_amdgcn_readfirstlane(count);
   q.len = __builtin_amdgcn_readfirstlane(len);
   q.row0 = __builtin_amdgcn_readfirstlane(row0);
   q.rows = __builtin_amdgcn_readfirstlane(rows);
+  q.all = __builtin_amdgcn_readfirstlane(all);
   q.total = __builtin_amdgcn_readfirstlane(total);
-  const int64_t first = q.count == 1 ? 0 : (int64_t)(w - q.slot0) * per * step;
-  q.first = __builtin_amdgcn_readfirstlane((int)min(first, (int64_t)q.total));
-  q.last = __builtin_amdgcn_readfirstlane(q.count == 1 ? q.total : (int)min(first + (int64_t)per * step, (int64_t)q.total));
+  const int64_t i = w - q.slot0;
+  q.first = q.count == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(i * steps / q.count) * step);
+  q.last = q.count == 1 ? q.total : __builtin_amdgcn_readfirstlane((int)min((i + 1) * steps / q.count * step, (int64_t)q.total));
   return true;
 }
 
@@ -257,30 +285,34 @@ __device__ __forceinline__ float row_max(float v) {
   return fmaxf(v, __shfl_xor(v, 32, kWave));
 }
 
-// q, out: [n_rows][H dh]; tree: [n_rows] or null; part: [slots][Hkv][row blocks x 16 QT][DH] and pml: the same rows x {reference in log2,
-// sum} for sequences of more than one slot, whose {first slot, count} go to slot_of [n_seqs][2].
+// q, out: [n_rows][H dh]; tree: [n_rows] or null; part: [slots][Hkv][prows][DH] and pml: the same rows x {reference in log2,
+// sum} for sequences of more than one slot, whose rows' {first slot, slots, row in the sequence} go to row_slot [n_rows][4].
+// NW waves; SHARED: every wave has 16 QT query rows of its own and all of them read the same tiles, else all have the same rows and tiles of their own.
 // grid: 8 ceil(slots Hkv / 8) blocks; workgroup b belongs to XCD b % 8, and the row blocks that read the same keys stay on one
 // XCD, one behind the other.
-template <typename T, int DH, int QT, int S>
-__global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
-                                                                     const unsigned long long* __restrict__ tree, KvView c,
-                                                                     T* __restrict__ out, float* __restrict__ part, float* __restrict__ pml,
-                                                                     int32_t* __restrict__ slot_of, int H, int Hkv, int dh, int max_rows,
-                                                                     int slots, int spare, int blocks, float scale_log2e) {
+template <typename T, int DH, int QT, int NW, bool SHARED, int S>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DH == 128 && QT == 2 ? 1 : 2))) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
+                                                               const unsigned long long* __restrict__ tree, KvView c,
+                                                               T* __restrict__ out, float* __restrict__ part, float* __restrict__ pml,
+                                                               int4* __restrict__ row_slot, int H, int Hkv, int dh, int max_rows,
+                                                               int slots, int spare, int blocks, float scale_log2e) {
   typedef KvTile<T, DH> L;
   constexpr bool BF = L::BF;
-  constexpr int KEYS = L::KEYS, ROWS = 16 * QT, NT = DH < 64 ? 4 : DH / 16, KS = BF ? DH / 32 : DH / 16, NS = KEYS / 4 / 4;
-  constexpr int STAGE = 2 * L::BYTES, NCOPY = 2 * L::COPIES;
-  extern __shared__ __align__(16) unsigned char smem[];      // [waves][S][STAGE]; then [waves][ROWS][DH] fp32 and [waves][ROWS][2]
+  constexpr int KEYS = L::KEYS, ROWS = 16 * QT, NT = DH < 64 ? 4 : DH / 16, KS = BF ? DH / 32 : DH / 16, NS = KEYS / 16;
+  constexpr int BLOCK_ROWS = SHARED ? NW * ROWS : ROWS, TILE_WAVES = SHARED ? 1 : NW;
+  constexpr int STAGE = 2 * L::BYTES, NCOPY = 2 * L::COPIES / (SHARED ? NW : 1);       // copies of a wave per tile
+  static_assert(NCOPY * (SHARED ? NW : 1) == 2 * L::COPIES, "every wave issues the same number of copies");
+  extern __shared__ __align__(16) unsigned char smem[];      // rings of S stages; then (not SHARED) [waves][ROWS][DH] fp32 and [waves][ROWS][2]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int xj = blockIdx.x >> 3, rb = xj % blocks, pair = (xj / blocks) * 8 + (blockIdx.x & 7);
   if (pair >= slots * Hkv) return;
   const int w = pair / Hkv, kvh = pair - w * Hkv, group = H / Hkv;
   KvSeq sq;
-  if (!kv_find_slot(c, max_rows, w, spare, KA_WAVES * KEYS, sq)) return;
-  if (spare && kvh == 0 && rb == 0 && threadIdx.x == 0 && w == sq.slot0) { slot_of[2 * sq.s] = w; slot_of[2 * sq.s + 1] = sq.count; }
-  const int q0 = rb * ROWS, nq = sq.rows * group;
-  if (q0 >= nq) return;
+  if (!kv_find_slot(c, max_rows, w, spare, KA_STEP, sq)) return;
+  if (spare && kvh == 0 && rb == 0 && w == sq.slot0)
+    for (int i = threadIdx.x; i < sq.all; i += NW * 64) row_slot[sq.row0 + i] = make_int4(w, i < sq.rows ? sq.count : 0, i, 0);
+  const int nq = sq.rows * group, q0 = rb * BLOCK_ROWS + (SHARED ? wave * ROWS : 0);
+  if (rb * BLOCK_ROWS >= nq) return;
 
   const int col = lane & 15, kg = lane >> 4;
   // ---- query rows: B operand, lane = row col, 16 bytes at chunk 4 ks + kg
@@ -305,30 +337,32 @@ __global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __
   }
   // keys past the last row of the block are of no use without a tree
   int last = sq.last;
-  if (!tree) last = __builtin_amdgcn_readfirstlane((int)min((int64_t)last, (int64_t)sq.len + (min(q0 + ROWS, nq) - 1) / group + 1));
+  if (!tree) last = __builtin_amdgcn_readfirstlane(min(last, sq.len + (min((rb + 1) * BLOCK_ROWS, nq) - 1) / group + 1));
   const kv_table_t table = (kv_table_t)(uintptr_t)(c.pages + (int64_t)sq.s * c.max_pages);
 
-  // ---- copies: lane -> 16 bytes of row lane / CHUNKS of a copy's RPC rows
-  const int crow = lane / L::CHUNKS, cchunk = lane % L::CHUNKS;
-  const unsigned char* ring = smem + wave * (S * STAGE);
-  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) const void*)ring;
+  // ---- copies: lane -> 16 bytes of row lane / CHUNKS of a copy's RPC rows.  Copy x of a tile: K, then V, 16-key halves in order;
+  // a wave that shares its tiles issues NCOPY of them.
   constexpr int PER = L::COPIES / KvHalves<T, DH>::N;       // copies of K, and of V, per 16-key half
-  unsigned vk[PER], vv[PER];                                // a lane's offsets from the half's base; the swizzles repeat every 16 rows
+  constexpr int NV = SHARED ? NCOPY : 2 * PER;              // a lane's offsets from the half's base; the swizzles repeat every 16 rows
+  const int crow = lane / L::CHUNKS, cchunk = lane % L::CHUNKS;
+  const unsigned char* ring = smem + (SHARED ? 0 : wave * (S * STAGE));
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) const void*)ring;
+  unsigned voff[NV];
 #pragma unroll
-  for (int x = 0; x < PER; ++x) {
-    const int row = x * L::RPC + crow;
-    int ck = cchunk ^ L::swz_k(row), cv = cchunk ^ L::swz_v(row);
-    if (!BF && ck * 16 >= dh * 4) ck = 0;                   // padding of a short row: anything inside it
-    if (!BF && cv * 16 >= dh * 4) cv = 0;
-    vk[x] = (unsigned)(row * dh * (int)sizeof(T) + ck * 16);
-    vv[x] = (unsigned)(row * dh * (int)sizeof(T) + cv * 16);
+  for (int x = 0; x < NV; ++x) {
+    const int y = SHARED ? wave * NCOPY + x : (x / PER) * L::COPIES + x % PER;
+    const int row = (y % PER) * L::RPC + crow;
+    int chunk = cchunk ^ (y < L::COPIES ? L::swz_k(row) : L::swz_v(row));
+    if (!BF && chunk * 16 >= dh * 4) chunk = 0;             // padding of a short row: anything inside it
+    voff[x] = (unsigned)(row * dh * (int)sizeof(T) + chunk * 16);
   }
   auto issue = [&](const KvHalves<T, DH>& hv, int stage) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < L::COPIES; ++x) {
-      const int64_t off = hv.off[x / PER] * (int)sizeof(T);
-      lds_copy16((const char*)kc + off, vk[x % PER], lds0 + stage * STAGE + x * 1024);
-      lds_copy16((const char*)vc + off, vv[x % PER], lds0 + stage * STAGE + L::BYTES + x * 1024);
+    for (int x = 0; x < NCOPY; ++x) {
+      const int y = SHARED ? wave * NCOPY + x : x, z = y % L::COPIES;
+      const bool is_v = y >= L::COPIES;
+      const int64_t off = (KvHalves<T, DH>::N == 1 || z / PER == 0 ? hv.off[0] : hv.off[KvHalves<T, DH>::N - 1]) * (int)sizeof(T);
+      lds_copy16((const char*)(is_v ? vc : kc) + off, voff[SHARED ? x : (y / L::COPIES) * PER + z % PER], lds0 + stage * STAGE + y * 1024);
     }
   };
 
@@ -342,7 +376,7 @@ __global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __
     for (int n = 0; n < NT; ++n) o[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int key_first = sq.first + wave * KEYS, stride = KA_WAVES * KEYS;
+  const int key_first = sq.first + (SHARED ? 0 : wave * KEYS), stride = TILE_WAVES * KEYS;
   const int n = last > key_first ? (last - key_first + stride - 1) / stride : 0;
   unsigned have[S];
 #pragma unroll
@@ -362,13 +396,12 @@ __global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __
     unsigned bad = 0;       // keys whose values are not finite and not everybody's
     if (edge) {
       // Values that nobody sees become zero, since 0 x NaN is not; of the call's own keys, which some rows see, those with a value that
-      // is not finite are taken out of the product and added row by row below.
+      // is not finite are taken out of the product and added row by row below.  (Waves that share the tile look first, all of them, then clear.)
 #pragma unroll
       for (int x = 0; x < L::COPIES; ++x) {
         const int row = x * L::RPC + crow, key = key0 + row;
         const bool none = !((exist >> row) & 1);
-        uint4* at = (uint4*)(Vt + x * 1024 + lane * 16);
-        const uint4 v = *at;
+        const uint4 v = *(const uint4*)(Vt + x * 1024 + lane * 16);
         bool odd = false;
         if (key >= sq.len && !none) {
           const unsigned u[4] = {v.x, v.y, v.z, v.w};
@@ -382,10 +415,17 @@ __global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __
           bad |= 1u << (x * L::RPC + r);
           odd_lanes &= ~(((1ull << L::CHUNKS) - 1) << (r * L::CHUNKS));
         }
-        if (none || ((bad >> row) & 1)) *at = make_uint4(0, 0, 0, 0);
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if constexpr (SHARED) __syncthreads();
+#pragma unroll
+      for (int x = 0; x < L::COPIES; ++x) {
+        const int row = x * L::RPC + crow;
+        if (!((exist >> row) & 1) || ((bad >> row) & 1)) *(uint4*)(Vt + x * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+      }
+      if constexpr (SHARED) __syncthreads();
+      else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    if (SHARED && q0 >= nq) return;       // a wave without rows only copies
     // ---- fragments: K rows (A operand, lane = key row col), V transposed (A operand, lane = dimension)
     frag_t kf[NS][KS], vf[BF ? NT : 4 * ((NT + 3) / 4)];
 #pragma unroll
@@ -515,20 +555,27 @@ __global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __
   };
 
   __builtin_amdgcn_s_waitcnt(0x0F70);       // query rows and first tiles: no wait of the compiler's is left for the loop
-  // ---- the wave's tiles: S - 1 of them in flight while one is worked on
+  // ---- the tiles: S - 1 of them in flight while one is worked on (S - 2 at the barrier of waves that share them, which also says
+  // that the oldest stage has been read)
   int stage = 0;
   KvHalves<T, DH> nx;
   if (S - 1 < n) nx = kv_halves<T, DH>(c, table, key_first + (S - 1) * stride, sq.total, kvh, dh);
   for (int it = 0; it < n; ++it) {
-    if (it + S - 1 < n) {
+    auto next = [&]() __attribute__((always_inline)) {
       int into = stage + S - 1;
       into = into >= S ? into - S : into;
       have[S - 1] = nx.have;
       issue(nx, into);
       if (it + S < n) nx = kv_halves<T, DH>(c, table, key_first + (it + S) * stride, sq.total, kvh, dh);
+    };
+    if constexpr (SHARED) {
+      if (it + S - 2 < n) wait_copies<(S - 2) * NCOPY>();
+      else wait_copies<0>();
+      __syncthreads();
+      if (it + S - 1 < n) next();
+    } else if (it + S - 1 < n) {
+      next();
       wait_copies<(S - 1) * NCOPY>();
-    } else if (S > 2 && it + S - 2 < n) {
-      wait_copies<(S > 2 ? S - 2 : 0) * NCOPY>();
     } else {
       wait_copies<0>();
     }
@@ -538,178 +585,209 @@ __global__ __launch_bounds__(KA_WAVES * 64) void kv_attention_kernel(const T* __
     stage = stage + 1 == S ? 0 : stage + 1;
   }
 
-  // ---- join the waves: rows of O (fp32) and {reference, sum} in LDS
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     lsum[t] += __shfl_xor(lsum[t], 16, kWave);
     lsum[t] += __shfl_xor(lsum[t], 32, kWave);
   }
-  __syncthreads();
-  float* Os = (float*)smem;
-  float* ML = Os + KA_WAVES * ROWS * DH;
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    float* r = Os + (size_t)(wave * ROWS + t * 16 + col) * DH;
-    if constexpr (BF) {
-#pragma unroll
-      for (int d = 0; d < NT; ++d) *(f32x4*)(r + d * 16 + kg * 4) = o[t][d];
-    } else {
-#pragma unroll
-      for (int b = 0; b < (NT + 3) / 4; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int dim = b * 64 + kg * 16 + e * 4;
-          if (dim < DH) *(f32x4*)(r + dim) = f32x4{o[t][b * 4][e], o[t][b * 4 + 1][e], o[t][b * 4 + 2][e], o[t][b * 4 + 3][e]};
-        }
-    }
-    if (kg == 0) { ML[(wave * ROWS + t * 16 + col) * 2] = m2[t]; ML[(wave * ROWS + t * 16 + col) * 2 + 1] = lsum[t]; }
-  }
-  __syncthreads();
   const bool whole = sq.count == 1;
-  for (int x = threadIdx.x; x < ROWS * (DH / 4); x += KA_WAVES * 64) {
-    const int r = x / (DH / 4), d = (x - r * (DH / 4)) * 4, qi = q0 + r;
-    if (qi >= nq || d >= dh) continue;
-    float ref = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < KA_WAVES; ++v) ref = fmaxf(ref, ML[(v * ROWS + r) * 2]);
-    float sum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int v = 0; v < KA_WAVES; ++v) {
-      const float mv = ML[(v * ROWS + r) * 2], f = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - ref);
-      const f32x4 ov = *(const f32x4*)(Os + (size_t)(v * ROWS + r) * DH + d);
-      if (mv == -INFINITY) continue;       // a wave without a visible key
-      sum = fmaf(f, ML[(v * ROWS + r) * 2 + 1], sum);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, ov[e], acc[e]);
-    }
+  // four dimensions of a row: to out, or as they are to the slot's place
+  auto store = [&](int qi, int d, const f32x4& acc, float ref, float sum) __attribute__((always_inline)) {
     if (whole) {
       const float inv = ref == -INFINITY ? 0.f : 1.f / sum;       // a row that sees nothing is zero
       const int i = qi / group, g = qi - i * group;
-      T* dst = out + (int64_t)(sq.row0 + i) * (H * dh) + (kvh * group + g) * dh + d;
       Pack<T, 4> v4;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v4.v[e] = from_f32<T>(ref == -INFINITY ? 0.f : acc[e] * inv);
-      *(Pack<T, 4>*)dst = v4;
+      *(Pack<T, 4>*)(out + (int64_t)(sq.row0 + i) * (H * dh) + (kvh * group + g) * dh + d) = v4;
     } else {
-      const int64_t at = ((int64_t)w * Hkv + kvh) * (blocks * ROWS) + qi;
+      const int64_t at = ((int64_t)w * Hkv + kvh) * (blocks * BLOCK_ROWS) + qi;
       *(f32x4*)(part + at * DH + d) = acc;
       if (d == 0) { pml[at * 2] = ref; pml[at * 2 + 1] = sum; }
+    }
+  };
+  auto dims = [&](int t, int x) __attribute__((always_inline)) {       // the x-th four consecutive dimensions of a lane
+    if constexpr (BF) return o[t][x];
+    else return f32x4{o[t][x / 4 * 4][x % 4], o[t][x / 4 * 4 + 1][x % 4], o[t][x / 4 * 4 + 2][x % 4], o[t][x / 4 * 4 + 3][x % 4]};
+  };
+  auto dim_of = [&](int x) __attribute__((always_inline)) { return BF ? x * 16 + kg * 4 : x / 4 * 64 + kg * 16 + x % 4 * 4; };
+  if constexpr (SHARED) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int qi = q0 + t * 16 + col;
+      if (qi < nq)
+#pragma unroll
+        for (int x = 0; x < NT; ++x) store(qi, dim_of(x), dims(t, x), m2[t], lsum[t]);
+    }
+  } else {
+    // ---- join the waves: rows of O (fp32) and {reference, sum} in LDS
+    __syncthreads();
+    float* Os = (float*)smem;
+    float* ML = Os + NW * ROWS * DH;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float* r = Os + (size_t)(wave * ROWS + t * 16 + col) * DH;
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+        if (dim_of(x) < DH) *(f32x4*)(r + dim_of(x)) = dims(t, x);
+      if (kg == 0) { ML[(wave * ROWS + t * 16 + col) * 2] = m2[t]; ML[(wave * ROWS + t * 16 + col) * 2 + 1] = lsum[t]; }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < ROWS * (DH / 4); x += NW * 64) {
+      const int r = x / (DH / 4), d = (x - r * (DH / 4)) * 4, qi = q0 + r;
+      if (qi >= nq || d >= dh) continue;
+      float ref = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < NW; ++v) ref = fmaxf(ref, ML[(v * ROWS + r) * 2]);
+      float sum = 0.f;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float mv = ML[(v * ROWS + r) * 2], f = __builtin_amdgcn_exp2f(mv - ref);
+        if (mv == -INFINITY) continue;       // a wave without a visible key
+        const f32x4 ov = *(const f32x4*)(Os + (size_t)(v * ROWS + r) * DH + d);
+        sum = fmaf(f, ML[(v * ROWS + r) * 2 + 1], sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, ov[e], acc[e]);
+      }
+      store(qi, d, acc, ref, sum);
     }
   }
 }
 
-// Rows of sequences that were cut into several slots: the slots' results joined.  grid: (n_rows, H), block: 64.
-template <typename T>
-__global__ __launch_bounds__(64) void kv_join_kernel(KvView c, T* __restrict__ out, const float* __restrict__ part, const float* __restrict__ pml,
-                                                     const int32_t* __restrict__ slot_of, int H, int Hkv, int dh, int DH, int max_rows,
-                                                     int prows) {
-  const int lane = threadIdx.x, h = blockIdx.y, group = H / Hkv, kvh = h / group;
-  const int64_t row = blockIdx.x;
-  int s = -1;
-  for (int b = 0; b < c.n_seqs && s < 0; b += 64) {
-    const bool mine = b + lane < c.n_seqs && row >= c.row_start[b + lane] && row < c.row_start[b + lane + 1];
-    const unsigned long long hit = __ballot(mine);
-    if (hit) s = b + __ffsll(hit) - 1;
-  }
-  if (s < 0) return;
-  const int i = (int)(row - max(c.row_start[s], 0));
-  const int slot = slot_of[2 * s], count = slot_of[2 * s + 1];
-  if (count <= 1 || i >= max_rows) return;
+// Rows of sequences that were cut into several slots: the slots' results joined, one wave per row and head.  DH / 4 lanes hold a slot's
+// row, so 64 / (DH / 4) slots are read at a time.  grid: ceil(n_rows H / 4), block: 256.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvView c, T* __restrict__ out, const float* __restrict__ part, const float* __restrict__ pml,
+                                                      const int4* __restrict__ row_slot, int H, int Hkv, int dh, int max_rows, int slots, int prows) {
+  constexpr int LANES = DH / 4, TOGETHER = 64 / LANES;
+  const int lane = threadIdx.x & 63, sub = lane / LANES, d = lane % LANES * 4, group = H / Hkv;
+  const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), row = x / H;
+  const int h = (int)(x - row * H), kvh = h / group;
+  if (row >= c.n_rows) return;
+  const int4 rs = row_slot[row];
+  // rows outside [row_start[0], row_start[n_seqs]) are nobody's, and nobody has written their entry; no entry leads outside the slots
+  if (row < c.row_start[0] || row >= c.row_start[c.n_seqs]) return;
+  const int slot = rs.x, count = rs.y, i = rs.z;
+  if (count <= 1 || slot < 0 || count > slots - slot || i < 0 || i >= max_rows) return;
   const int64_t at0 = ((int64_t)slot * Hkv + kvh) * prows + i * group + (h - kvh * group), step = (int64_t)Hkv * prows;
   float ref = -INFINITY;
   for (int n = lane; n < count; n += 64) ref = fmaxf(ref, pml[(at0 + n * step) * 2]);
+  float sum = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   ref = wave_max(ref);
-  float sum = 0.f, acc0 = 0.f, acc1 = 0.f;
 #pragma unroll 4
-  for (int n = 0; n < count; ++n) {
+  for (int n = sub; n < count; n += TOGETHER) {
     const int64_t at = at0 + n * step;
     const float m = pml[at * 2], l = pml[at * 2 + 1];
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref);
-    const float a = lane < dh ? part[at * DH + lane] : 0.f, b = lane + 64 < dh ? part[at * DH + lane + 64] : 0.f;
-    if (m == -INFINITY) continue;
-    sum = fmaf(f, l, sum);
-    acc0 = fmaf(f, a, acc0);
-    acc1 = fmaf(f, b, acc1);
+    const f32x4 v = d < dh ? *(const f32x4*)(part + at * DH + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    const bool some = m != -INFINITY;       // (a slot whose keys the row does not see)
+    sum = some ? fmaf(f, l, sum) : sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = some ? fmaf(f, v[e], acc[e]) : acc[e];
   }
-  const float inv = ref == -INFINITY ? 0.f : 1.f / sum;
-  T* dst = out + row * (int64_t)(H * dh) + h * dh;
-  if (lane < dh) dst[lane] = from_f32<T>(ref == -INFINITY ? 0.f : acc0 * inv);
-  if (lane + 64 < dh) dst[lane + 64] = from_f32<T>(ref == -INFINITY ? 0.f : acc1 * inv);
+#pragma unroll
+  for (int o = LANES; o < 64; o <<= 1) {
+    sum += __shfl_xor(sum, o, kWave);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, kWave);
+  }
+  if (sub || d >= dh) return;
+  Pack<T, 4> v4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v4.v[e] = from_f32<T>(ref == -INFINITY ? 0.f : acc[e] / sum);
+  *(Pack<T, 4>*)(out + row * (int64_t)(H * dh) + h * dh + d) = v4;
 }
 
 // Shape of a launch, from what the host knows (the lengths are on the device).
 struct KvPlan {
-  int DH, QT, blocks, slots, spare;
-  size_t part, pml, slot_of, total;         // workspace
+  int DH, QT, NW, blocks, slots, spare, prows;
+  bool shared;
+  size_t part, pml, row_slot, total;         // workspace
 };
 
-constexpr int KA_TARGET = 512;              // workgroups wanted: two per compute unit
-
-inline KvPlan kv_plan(bool bf, int n_seqs, int max_rows, int64_t max_keys, int H, int Hkv, int dh) {
+inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max_keys, int H, int Hkv, int dh) {
   KvPlan p;
   p.DH = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
   const int64_t nq = (int64_t)max_rows * (H / Hkv);
   p.QT = nq <= 16 ? 1 : nq <= 32 || p.DH == 128 || !bf ? 2 : 4;
-  p.blocks = (int)((nq + 16 * p.QT - 1) / (16 * p.QT));
-  const int64_t step = KA_WAVES * (bf ? 32 : 16);
+  p.NW = 4;
+  p.shared = bf && nq > 16 * p.QT;
+  if (p.shared) {
+    p.QT = p.DH == 128 && nq <= 64 ? 1 : 2;
+    p.NW = nq <= 128 ? 4 : 8;
+  }
+  const int rows = 16 * p.QT * (p.shared ? p.NW : 1);
+  p.blocks = (int)((nq + rows - 1) / rows);
+  const int64_t steps = (max_keys + KA_STEP - 1) / KA_STEP;
   int64_t spare = KA_TARGET / ((int64_t)Hkv * p.blocks);
-  const int64_t most = n_seqs * ((max_keys + step - 1) / step - 1);       // cuts that keys could be made at
-  if (spare > most) spare = most;
+  if (spare > n_seqs * (steps - 1)) spare = n_seqs * (steps - 1);         // cuts that keys could be made at
   p.spare = (int)(spare < 0 ? 0 : spare);
   p.slots = n_seqs + p.spare;
+  p.prows = p.blocks * rows;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  const size_t rows = p.spare ? (size_t)p.slots * Hkv * p.blocks * 16 * p.QT : 0;
+  const size_t all = p.spare ? (size_t)p.slots * Hkv * p.prows : 0;
   p.part = 0;
-  p.pml = up(rows * p.DH * 4);
-  p.slot_of = p.pml + up(rows * 8);
-  p.total = p.slot_of + (p.spare ? up((size_t)n_seqs * 8) : 0);
+  p.pml = up(all * p.DH * 4);
+  p.row_slot = p.pml + up(all * 8);
+  p.total = p.row_slot + (p.spare ? up((size_t)n_rows * 16) : 0);
   return p;
 }
 
-template <typename T, int DH, int QT, int S>
+template <typename T, int DH, int QT, int NW, bool SHARED, int S>
 hipError_t launch_kv_attention_as(const KvPlan& p, const void* q, const void* k, const void* v, const unsigned long long* tree, const KvView& c,
                                   void* out, char* ws, int H, int Hkv, int dh, int max_rows, hipStream_t st) {
   typedef KvTile<T, DH> L;
-  constexpr int ring = KA_WAVES * S * 2 * L::BYTES, join = KA_WAVES * 16 * QT * (DH + 2) * 4, lds = ring > join ? ring : join;
+  constexpr int ring = (SHARED ? 1 : NW) * S * 2 * L::BYTES, join = SHARED ? 0 : NW * 16 * QT * (DH + 2) * 4, lds = ring > join ? ring : join;
   static std::atomic<uint64_t> raised{0};
   if (lds > 65536) {
-    const hipError_t e = raise_lds_limit((const void*)kv_attention_kernel<T, DH, QT, S>, lds, raised);
+    const hipError_t e = raise_lds_limit((const void*)kv_attention_kernel<T, DH, QT, NW, SHARED, S>, lds, raised);
     if (e != hipSuccess) return e;
   }
   const int64_t grid = 8 * (((int64_t)p.slots * Hkv + 7) / 8) * p.blocks;
-  kv_attention_kernel<T, DH, QT, S><<<(unsigned)grid, KA_WAVES * 64, lds, st>>>(
-      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, (float*)(ws + p.part), (float*)(ws + p.pml), (int32_t*)(ws + p.slot_of), H,
-      Hkv, dh, max_rows, p.slots, p.spare, p.blocks, 1.4426950408889634f / sqrtf((float)dh));
+  float *part = (float*)(ws + p.part), *pml = (float*)(ws + p.pml);
+  int4* row_slot = (int4*)(ws + p.row_slot);
+  kv_attention_kernel<T, DH, QT, NW, SHARED, S><<<(unsigned)grid, NW * 64, lds, st>>>(
+      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, part, pml, row_slot, H, Hkv, dh, max_rows, p.slots, p.spare, p.blocks,
+      1.4426950408889634f / sqrtf((float)dh));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.spare) return e;
-  kv_join_kernel<T><<<dim3((unsigned)c.n_rows, H), 64, 0, st>>>(c, (T*)out, (const float*)(ws + p.part), (const float*)(ws + p.pml),
-                                                              (const int32_t*)(ws + p.slot_of), H, Hkv, dh, DH, max_rows, p.blocks * 16 * QT);
+  kv_join_kernel<T, DH><<<(unsigned)(((int64_t)c.n_rows * H + 3) / 4), 256, 0, st>>>(c, (T*)out, part, pml, row_slot, H, Hkv, dh, max_rows, p.slots, p.prows);
   return hipGetLastError();
 }
 
 inline hipError_t launch_kv_attention(bool bf, const KvPlan& p, const void* q, const void* k, const void* v, const unsigned long long* tree,
                                       const KvView& c, void* out, char* ws, int H, int Hkv, int dh, int max_rows, hipStream_t st) {
-#define ARMT_KA(T, D, Q, S) return launch_kv_attention_as<T, D, Q, S>(p, q, k, v, tree, c, out, ws, H, Hkv, dh, max_rows, st)
+#define ARMT_KA(T, D, Q, N, SH, S) return launch_kv_attention_as<T, D, Q, N, SH, S>(p, q, k, v, tree, c, out, ws, H, Hkv, dh, max_rows, st)
+  if (bf && p.shared) {
+    if (p.DH == 64) {
+      if (p.NW == 4) ARMT_KA(bf16, 64, 2, 4, true, 4);
+      ARMT_KA(bf16, 64, 2, 8, true, 4);
+    }
+    if (p.QT == 1) ARMT_KA(bf16, 128, 1, 4, true, 4);
+    if (p.NW == 4) ARMT_KA(bf16, 128, 2, 4, true, 4);
+    ARMT_KA(bf16, 128, 2, 8, true, 4);
+  }
   if (bf) {
     if (p.DH == 64) {
-      if (p.QT == 1) ARMT_KA(bf16, 64, 1, 2);
-      if (p.QT == 2) ARMT_KA(bf16, 64, 2, 2);
-      ARMT_KA(bf16, 64, 4, 2);
+      if (p.QT == 1) ARMT_KA(bf16, 64, 1, 4, false, 2);
+      if (p.QT == 2) ARMT_KA(bf16, 64, 2, 4, false, 2);
+      ARMT_KA(bf16, 64, 4, 4, false, 2);
     }
-    if (p.QT == 1) ARMT_KA(bf16, 128, 1, 2);
-    ARMT_KA(bf16, 128, 2, 2);
+    if (p.QT == 1) ARMT_KA(bf16, 128, 1, 4, false, 2);
+    ARMT_KA(bf16, 128, 2, 4, false, 2);
   }
   if (p.DH == 32) {
-    if (p.QT == 1) ARMT_KA(float, 32, 1, 2);
-    ARMT_KA(float, 32, 2, 2);
+    if (p.QT == 1) ARMT_KA(float, 32, 1, 4, false, 2);
+    ARMT_KA(float, 32, 2, 4, false, 2);
   }
   if (p.DH == 64) {
-    if (p.QT == 1) ARMT_KA(float, 64, 1, 2);
-    ARMT_KA(float, 64, 2, 2);
+    if (p.QT == 1) ARMT_KA(float, 64, 1, 4, false, 2);
+    ARMT_KA(float, 64, 2, 4, false, 2);
   }
-  if (p.QT == 1) ARMT_KA(float, 128, 1, 2);
-  ARMT_KA(float, 128, 2, 2);
+  if (p.QT == 1) ARMT_KA(float, 128, 1, 4, false, 2);
+  ARMT_KA(float, 128, 2, 4, false, 2);
 #undef ARMT_KA
 }
 

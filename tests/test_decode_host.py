@@ -50,7 +50,7 @@ def test_configuration_refusals(lib, kw, status):
     c, k = cfg(**kw), cache()
     assert lib.armt_kv_append(C.byref(c), C.byref(k), FAKE, 48 * 64, 5, None, FAKE, None) == status
     assert lib.armt_kv_attention(C.byref(c), C.byref(k), FAKE, 5, 3, None, FAKE, FAKE, 1 << 40, None) == status
-    assert lib.armt_kv_attention_workspace_bytes(C.byref(c), 2, 4, 64, 3) == 0
+    assert lib.armt_kv_attention_workspace_bytes(C.byref(c), 2, 4, 64, 5, 3) == 0
 
 
 def test_fp32_head_sizes(lib):
@@ -71,7 +71,7 @@ def test_append_refusals(lib):
 
 def test_attention_refusals(lib):
     c, k = cfg(), cache()
-    need = lib.armt_kv_attention_workspace_bytes(C.byref(c), 2, 4, 64, 3)
+    need = lib.armt_kv_attention_workspace_bytes(C.byref(c), 2, 4, 64, 5, 3)
     assert need >= 256
 
     def call(q=FAKE, n=5, rows=3, tree=None, out=FAKE, ws=FAKE, size=need):
@@ -87,9 +87,9 @@ def test_attention_refusals(lib):
 def test_attention_workspace(lib):
     c = cfg()
     size = lambda *a: lib.armt_kv_attention_workspace_bytes(C.byref(c), *a)  # noqa: E731
-    assert all(size(*a) == 0 for a in ((0, 4, 64, 1), (2, 0, 64, 1), (2, 4, 0, 1), (2, 4, 64, 0), (65537, 4, 64, 1)))
-    assert 0 < size(1, 1, 16, 1) <= 1 << 16                                    # keys of one step: nothing is cut
-    assert size(1, 1, 16, 1) <= size(1, 16384, 64, 1) < 64 << 20 and size(256, 16384, 64, 64) < 2 << 30
+    assert all(size(*a) == 0 for a in ((0, 4, 64, 1, 1), (2, 0, 64, 1, 1), (2, 4, 0, 1, 1), (2, 4, 64, 0, 1), (2, 4, 64, 1, 0), (65537, 4, 64, 1, 1)))
+    assert 0 < size(1, 1, 16, 1, 1) <= 1 << 16                                    # keys of one step: nothing is cut
+    assert size(1, 1, 16, 1, 1) <= size(1, 16384, 64, 1, 1) < 64 << 20 and size(256, 16384, 64, 256 * 64, 64) < 2 << 30
 
 
 def test_beam_select_refusals(lib):

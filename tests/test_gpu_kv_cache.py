@@ -98,6 +98,12 @@ ATTEND = [
     ("3b", "bf16", 32, [200, 31], [1, 1], False),
     ("3b", "bf16", 64, [260, 3, 0], [23, 64, 2], True),
     ("8b", "bf16", 256, [515], [3], False),
+    ("3b", "bf16", 32, [300, 60], [10, 4], True),
+    ("3b", "bf16", 32, [300, 0], [20, 9], True),
+    ("3b", "bf16", 16, [131, 64], [40, 33], False),
+    ("8b", "bf16", 64, [40], [90], False),
+    ("one", "bf16", 64, [1000, 1], [16, 3], True),
+    ("8b", "f32", 16, [40], [9], True),
     ("tiny", "f32", 16, [0, 1, 15, 16, 64, 65, 300], [1] * 7, False),
     ("tiny", "f32", 16, [40, 0, 90], [7, 33, 12], True),
     ("narrow", "f32", 32, [50, 7], [9, 2], True),
