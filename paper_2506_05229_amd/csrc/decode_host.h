@@ -27,7 +27,7 @@ armt_status check_cache(const armt_config* cfg, const armt_kv_cache* cache, int3
 bool attention_plan(const Dims& D, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t n_rows, int32_t max_rows, KvPlan* p) {
   if ((int64_t)max_rows * (D.H / D.Hkv) > 1 << 30) return false;
   *p = kv_plan(D.bf16, n_seqs, n_rows, max_rows, (int64_t)max_pages * page_len, D.H, D.Hkv, D.dh);
-  return 8 * (((int64_t)p->slots * D.Hkv + 7) / 8) * p->blocks <= 0x7fffffff && (int64_t)n_rows * D.H <= 0x7fffffff;
+  return kv_grid(*p, D.Hkv) <= 0x7fffffff && (int64_t)n_rows * D.H <= 0x7fffffff;
 }
 
 // Whether two sets of n rows may share memory (rows of equal stride may lie between each other).

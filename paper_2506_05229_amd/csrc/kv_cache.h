@@ -130,8 +130,9 @@ inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const K
 // query row, so the softmax needs no exchange until a reference has to move), P^T stays in the registers in which the second
 // product wants it, and V, which that product wants with the keys side by side, is read from its rows by transposing LDS reads.
 // Reading every key and value once bounds it for up to about 64 query rows.
+constexpr int KA_WAVES = 4;
 constexpr int KA_STEP = 128;              // keys are cut into slots at multiples of this
-constexpr int KA_TARGET = 512;            // workgroups wanted: two per compute unit
+constexpr int KA_CUS = 256;               // compute units
 constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
 
 struct KvSeq { int s, len, row0, rows, all, total, first, last, count, slot0; };   // keys of a slot: [first, last)
@@ -175,12 +176,18 @@ __device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int 
       load(min(b + lane, c.n_seqs - 1));
       sum += __builtin_amdgcn_readlane(wave_scan(b + lane < c.n_seqs ? steps : 0), 63);
     }
-    const int per = sum > 0x7fff0000 - spare ? 0x7fffffff : max(1, ((int)sum + spare - 1) / spare);
+    unsigned per = sum > 0x7fff0000 - spare ? 0x7fffffffu : max(1u, ((unsigned)sum + spare - 1) / (unsigned)spare);
+    auto slots_of = [&]() __attribute__((always_inline)) { return steps > 0 ? (int)((unsigned)(steps - 1) / per) + 1 : 1; };
+    // few long sequences: no more slots than `spare`, which fill the chip once (3 x 131072 keys in 264 workgroups of which 8 wait for a second
+    // round: 194 us, in 256: 151; the loop ends: per grows, and n_seqs slots fit)
+    if (c.n_seqs <= 64 && c.n_seqs * 4 <= spare)
+      for (int over; (over = __builtin_amdgcn_readlane(wave_scan(lane < c.n_seqs ? slots_of() : 0), 63) - spare) > 0;)
+        per += max(1u, (unsigned)((uint64_t)per * over / (2u * spare)));
     int before = 0;
     s = -1;
     for (int b = 0; b < c.n_seqs; b += 64) {
       if (c.n_seqs > 64) load(min(b + lane, c.n_seqs - 1));
-      const int n = b + lane < c.n_seqs ? max(1, (int)(((int64_t)steps + per - 1) / per)) : 0;
+      const int n = b + lane < c.n_seqs ? slots_of() : 0;
       const int upto = wave_scan(n), start = before + upto - n;
       const unsigned long long hit = __ballot(w >= start && w < start + n);
       if (hit) {
@@ -208,9 +215,14 @@ __device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int 
   q.rows = __builtin_amdgcn_readfirstlane(rows);
   q.all = __builtin_amdgcn_readfirstlane(all);
   q.total = __builtin_amdgcn_readfirstlane(total);
-  const int64_t i = w - q.slot0;
-  q.first = q.count == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(i * steps / q.count) * step);
-  q.last = q.count == 1 ? q.total : __builtin_amdgcn_readfirstlane((int)min((i + 1) * steps / q.count * step, (int64_t)q.total));
+  // the first (steps % count) slots take one step more
+  q.first = 0;
+  q.last = q.total;
+  if (q.count > 1) {
+    const unsigned n = __builtin_amdgcn_readfirstlane(steps), i = w - q.slot0, base = n / (unsigned)q.count, more = n - base * q.count;
+    q.first = __builtin_amdgcn_readfirstlane((int)(i * base + min(i, more)) * step);
+    q.last = __builtin_amdgcn_readfirstlane(min(q.first + (int)(base + (i < more)) * step, q.total));
+  }
   return true;
 }
 
@@ -246,15 +258,26 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
   return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
 
+// The table's entries for a tile's halves, as they are: nothing waits for them before they are used, a tile later.
 template <typename T, int DH>
-__device__ __forceinline__ KvHalves<T, DH> kv_halves(const KvView& c, kv_table_t table, int key0, int total, int kvh, int dh) {
+struct KvEntries { int page[KvHalves<T, DH>::N], key0; };
+
+template <typename T, int DH>
+__device__ __forceinline__ KvEntries<T, DH> kv_entries(const KvView& c, kv_table_t table, int key0) {
+  KvEntries<T, DH> e;
+  e.key0 = key0;
+#pragma unroll
+  for (int h = 0; h < KvHalves<T, DH>::N; ++h) e.page[h] = table[min((key0 + 16 * h) >> c.page_shift, c.max_pages - 1)];
+  return e;
+}
+
+template <typename T, int DH>
+__device__ __forceinline__ KvHalves<T, DH> kv_halves(const KvView& c, const KvEntries<T, DH>& e, int total, int kvh, int dh) {
   KvHalves<T, DH> r;
   r.have = 0;
 #pragma unroll
   for (int h = 0; h < KvHalves<T, DH>::N; ++h) {
-    const int key = key0 + 16 * h;
-    const int j = min(key >> c.page_shift, c.max_pages - 1);
-    const int page = __builtin_amdgcn_readfirstlane(table[j]);
+    const int key = e.key0 + 16 * h, page = __builtin_amdgcn_readfirstlane(e.page[h]);
     const bool ok = key < total && page >= 0 && page < c.n_pages;
     r.have |= ok ? 1u << h : 0u;
     r.off[h] = uniform64((int64_t)(ok ? page : 0) * c.page_stride + (int64_t)((kvh << c.page_shift) + (key & ((1 << c.page_shift) - 1))) * dh);
@@ -287,32 +310,41 @@ __device__ __forceinline__ float row_max(float v) {
 
 // q, out: [n_rows][H dh]; tree: [n_rows] or null; part: [slots][Hkv][prows][DH] and pml: the same rows x {reference in log2,
 // sum} for sequences of more than one slot, whose rows' {first slot, slots, row in the sequence} go to row_slot [n_rows][4].
-// NW waves; SHARED: every wave has 16 QT query rows of its own and all of them read the same tiles, else all have the same rows and tiles of their own.
-// grid: 8 ceil(slots Hkv / 8) blocks; workgroup b belongs to XCD b % 8, and the row blocks that read the same keys stay on one
-// XCD, one behind the other.
-template <typename T, int DH, int QT, int NW, bool SHARED, int S>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DH == 128 && QT == 2 ? 1 : 2))) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
+// SHARED: every wave has 16 QT query rows of its own and all of them read the same tiles, else all have the same rows and tiles of their own.
+// grid: slots Hkv, or 8 ceil(slots Hkv / 8) blocks with more than one row block.  The heads of a slot run side by side: they share its pages (the
+// other way round, 48 sequences took 115 us instead of 107).  Workgroup b belongs to XCD b % 8: row blocks that read the same keys
+// stay on one XCD, one behind the other.
+template <typename T, int DH, int QT, bool SHARED, int S>
+__global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DH == 128 && QT == 2 ? 1 : 2))) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
                                                                const unsigned long long* __restrict__ tree, KvView c,
                                                                T* __restrict__ out, float* __restrict__ part, float* __restrict__ pml,
-                                                               int4* __restrict__ row_slot, int H, int Hkv, int dh, int max_rows,
-                                                               int slots, int spare, int blocks, float scale_log2e) {
+                                                               int4* __restrict__ row_slot, int H, int Hkv, int group, int dh, int max_rows,
+                                                               int slots, int spare, int blocks, int brows, float scale_log2e) {
   typedef KvTile<T, DH> L;
+  constexpr int NW = KA_WAVES;
   constexpr bool BF = L::BF;
   constexpr int KEYS = L::KEYS, ROWS = 16 * QT, NT = DH < 64 ? 4 : DH / 16, KS = BF ? DH / 32 : DH / 16, NS = KEYS / 16;
-  constexpr int BLOCK_ROWS = SHARED ? NW * ROWS : ROWS, TILE_WAVES = SHARED ? 1 : NW;
+  constexpr int TILE_WAVES = SHARED ? 1 : NW;
   constexpr int STAGE = 2 * L::BYTES, NCOPY = 2 * L::COPIES / (SHARED ? NW : 1);       // copies of a wave per tile
   static_assert(NCOPY * (SHARED ? NW : 1) == 2 * L::COPIES, "every wave issues the same number of copies");
   extern __shared__ __align__(16) unsigned char smem[];      // rings of S stages; then (not SHARED) [waves][ROWS][DH] fp32 and [waves][ROWS][2]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int xj = blockIdx.x >> 3, rb = xj % blocks, pair = (xj / blocks) * 8 + (blockIdx.x & 7);
-  if (pair >= slots * Hkv) return;
-  const int w = pair / Hkv, kvh = pair - w * Hkv, group = H / Hkv;
+  int pair = blockIdx.x, rb = 0;
+  if (blocks > 1) {
+    const int x = pair >> 3;
+    rb = x % blocks;
+    pair = (x / blocks) * 8 + (pair & 7);
+  }
+  const int w = pair / Hkv, kvh = pair - w * Hkv;
+  if (w >= slots) return;
   KvSeq sq;
   if (!kv_find_slot(c, max_rows, w, spare, KA_STEP, sq)) return;
   if (spare && kvh == 0 && rb == 0 && w == sq.slot0)
     for (int i = threadIdx.x; i < sq.all; i += NW * 64) row_slot[sq.row0 + i] = make_int4(w, i < sq.rows ? sq.count : 0, i, 0);
-  const int nq = sq.rows * group, q0 = rb * BLOCK_ROWS + (SHARED ? wave * ROWS : 0);
-  if (rb * BLOCK_ROWS >= nq) return;
+  const int q0 = rb * brows, nq = min(sq.rows * group, q0 + brows);       // query rows of the workgroup: [q0, nq)
+  if (q0 >= nq) return;
+  // 16-row tile t of a wave: waves that share the keys take the block's tiles in turn, so that a short block is spread over them
+  auto qtile = [&](int t) __attribute__((always_inline)) { return q0 + (SHARED ? t * NW + wave : t) * 16; };
 
   const int col = lane & 15, kg = lane >> 4;
   // ---- query rows: B operand, lane = row col, 16 bytes at chunk 4 ks + kg
@@ -321,7 +353,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   KvMask mask[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const int qi = q0 + t * 16 + col, i = qi / group, g = qi - i * group;
+    const int qi = qtile(t) + col, i = qi / group, g = qi - i * group;
     const bool live = qi < nq;
     const int64_t row = sq.row0 + (live ? i : 0);
     const T* p = q + row * (int64_t)(H * dh) + (kvh * group + g) * dh;
@@ -337,7 +369,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   }
   // keys past the last row of the block are of no use without a tree
   int last = sq.last;
-  if (!tree) last = __builtin_amdgcn_readfirstlane(min(last, sq.len + (min((rb + 1) * BLOCK_ROWS, nq) - 1) / group + 1));
+  if (!tree) last = __builtin_amdgcn_readfirstlane(min(last, sq.len + (nq - 1) / group + 1));
   const kv_table_t table = (kv_table_t)(uintptr_t)(c.pages + (int64_t)sq.s * c.max_pages);
 
   // ---- copies: lane -> 16 bytes of row lane / CHUNKS of a copy's RPC rows.  Copy x of a tile: K, then V, 16-key halves in order;
@@ -382,50 +414,53 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 #pragma unroll
   for (int x = 0; x < S - 1; ++x)
     if (x < n) {
-      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, table, key_first + x * stride, sq.total, kvh, dh);
+      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, kv_entries<T, DH>(c, table, key_first + x * stride), sq.total, kvh, dh);
       have[x] = hv.have;
       issue(hv, x);
     }
 
+  bool any_odd = false;       // values that are not finite were left out
   auto tile = [&](int it, int stage, unsigned pages_ok) __attribute__((always_inline)) {
     unsigned char* Kt = (unsigned char*)ring + stage * STAGE;
     unsigned char* Vt = Kt + L::BYTES;
     const int key0 = key_first + it * stride;
     const bool edge = key0 + KEYS > min(sq.len, last) || pages_ok != (1u << KvHalves<T, DH>::N) - 1;       // (uniform) some key is not everybody's
     const unsigned exist = keys_below(sq.total, key0) & ((pages_ok & 1 ? 0xffffu : 0u) | (pages_ok & 2 ? 0xffff0000u : 0u));
-    unsigned bad = 0;       // keys whose values are not finite and not everybody's
     if (edge) {
-      // Values that nobody sees become zero, since 0 x NaN is not; of the call's own keys, which some rows see, those with a value that
-      // is not finite are taken out of the product and added row by row below.  (Waves that share the tile look first, all of them, then clear.)
+      // Values of keys that do not exist become zero, since 0 x NaN is not.  So do, of the call's own keys, which some rows see and others do
+      // not, single values that are not finite: they are added to the rows that see them behind the loop.  (Waves that share
+      // the tile look first, all of them, then clear.)
+      const unsigned partly = exist & ~keys_below(sq.len, key0);
+      unsigned odd = 0;                  // bit x: not finite in copy x's 16 bytes
 #pragma unroll
       for (int x = 0; x < L::COPIES; ++x) {
-        const int row = x * L::RPC + crow, key = key0 + row;
-        const bool none = !((exist >> row) & 1);
         const uint4 v = *(const uint4*)(Vt + x * 1024 + lane * 16);
-        bool odd = false;
-        if (key >= sq.len && !none) {
-          const unsigned u[4] = {v.x, v.y, v.z, v.w};
+        const unsigned u[4] = {v.x, v.y, v.z, v.w};
+        bool no = false;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            odd |= BF ? (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u : (u[e] & 0x7f800000u) == 0x7f800000u;
-        }
-        unsigned long long odd_lanes = __ballot(odd);
-        while (odd_lanes) {
-          const int r = (__ffsll(odd_lanes) - 1) / L::CHUNKS;
-          bad |= 1u << (x * L::RPC + r);
-          odd_lanes &= ~(((1ull << L::CHUNKS) - 1) << (r * L::CHUNKS));
-        }
+        for (int e = 0; e < 4; ++e) no |= (BF && (u[e] & 0x7f80u) == 0x7f80u) | ((u[e] & 0x7f800000u) == 0x7f800000u);
+        odd |= no & ((partly >> (x * L::RPC + crow)) & 1) ? 1u << x : 0u;
       }
+      any_odd |= __ballot(odd != 0) != 0;
       if constexpr (SHARED) __syncthreads();
 #pragma unroll
       for (int x = 0; x < L::COPIES; ++x) {
-        const int row = x * L::RPC + crow;
-        if (!((exist >> row) & 1) || ((bad >> row) & 1)) *(uint4*)(Vt + x * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+        const bool none = !((exist >> (x * L::RPC + crow)) & 1);
+        if (none || ((odd >> x) & 1)) {
+          const uint4 v = *(const uint4*)(Vt + x * 1024 + lane * 16);
+          unsigned u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (none || (u[e] & 0x7f800000u) == 0x7f800000u) u[e] &= BF ? 0xffffu : 0u;
+            if (BF && (none || (u[e] & 0x7f80u) == 0x7f80u)) u[e] &= 0xffff0000u;
+          }
+          *(uint4*)(Vt + x * 1024 + lane * 16) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
       }
       if constexpr (SHARED) __syncthreads();
       else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    if (SHARED && q0 >= nq) return;       // a wave without rows only copies
+    if (SHARED && qtile(0) >= nq) return;       // a wave without rows only copies
     // ---- fragments: K rows (A operand, lane = key row col), V transposed (A operand, lane = dimension)
     frag_t kf[NS][KS], vf[BF ? NT : 4 * ((NT + 3) / 4)];
 #pragma unroll
@@ -462,6 +497,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
+      if (SHARED && t > 0 && qtile(t) >= nq) break;
       f32x4 sc[NS];
 #pragma unroll
       for (int a = 0; a < NS; ++a) {
@@ -475,10 +511,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
           }
         }
       }
-      unsigned seen = ~0u;
       if (edge) {
-        seen = keys_seen(mask[t], tree != nullptr, sq.len, key0);
-        const unsigned mine = (seen & exist) >> (kg * 4);
+        const unsigned mine = (keys_seen(mask[t], tree != nullptr, sq.len, key0) & exist) >> (kg * 4);
 #pragma unroll
         for (int a = 0; a < NS; ++a)
 #pragma unroll
@@ -529,44 +563,33 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[(d / 4) * 4 + r][d % 4], pr[0][r], o[t][d], 0, 0, 0);
       }
-      if (bad) {
-#pragma unroll
-        for (int a = 0; a < NS; ++a)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            for (int g = 0; g < 4; ++g) {
-              const int row = a * 16 + g * 4 + r;
-              if (!((bad >> row) & 1)) continue;
-              const int key = key0 + row;
-              const float p = __shfl(pr[a][r], g * 16 + col, kWave);
-              if (!((seen >> row) & 1)) continue;
-              const T* v = vc + (int64_t)table[key >> c.page_shift] * c.page_stride +
-                           (int64_t)((kvh << c.page_shift) + (key & ((1 << c.page_shift) - 1))) * dh;
-#pragma unroll
-              for (int d = 0; d < NT; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int dim = BF ? d * 16 + kg * 4 + e : (d / 4) * 64 + kg * 16 + e * 4 + d % 4;
-                  if (dim < dh) o[t][d][e] = fmaf(p, to_f32(v[dim]), o[t][d][e]);
-                }
-            }
-      }
     }
   };
 
-  __builtin_amdgcn_s_waitcnt(0x0F70);       // query rows and first tiles: no wait of the compiler's is left for the loop
+  // query rows and masks are here: a wait of the compiler's for them inside the loop would also wait for the copies in flight
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+      u32x4 r = __builtin_bit_cast(u32x4, qf[t][ks]);
+      asm volatile("" : "+v"(r));
+      qf[t][ks] = __builtin_bit_cast(frag_t, r);
+    }
+    asm volatile("" : "+v"(mask[t].bits), "+v"(mask[t].limit));
+  }
   // ---- the tiles: S - 1 of them in flight while one is worked on (S - 2 at the barrier of waves that share them, which also says
   // that the oldest stage has been read)
   int stage = 0;
-  KvHalves<T, DH> nx;
-  if (S - 1 < n) nx = kv_halves<T, DH>(c, table, key_first + (S - 1) * stride, sq.total, kvh, dh);
+  KvEntries<T, DH> nx = kv_entries<T, DH>(c, table, key_first + min(S - 1, n) * stride);
   for (int it = 0; it < n; ++it) {
     auto next = [&]() __attribute__((always_inline)) {
       int into = stage + S - 1;
       into = into >= S ? into - S : into;
-      have[S - 1] = nx.have;
-      issue(nx, into);
-      if (it + S < n) nx = kv_halves<T, DH>(c, table, key_first + (it + S) * stride, sq.total, kvh, dh);
+      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, nx, sq.total, kvh, dh);
+      have[S - 1] = hv.have;
+      issue(hv, into);
+      nx = kv_entries<T, DH>(c, table, key_first + (it + S) * stride);
     };
     if constexpr (SHARED) {
       if (it + S - 2 < n) wait_copies<(S - 2) * NCOPY>();
@@ -585,6 +608,26 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     stage = stage + 1 == S ? 0 : stage + 1;
   }
 
+  if (any_odd)
+    for (int x = 0; x < n * KEYS; ++x) {
+      const int key = key_first + x / KEYS * stride + x % KEYS;
+      if (key < sq.len || key >= sq.total) continue;
+      const int page = table[min(key >> c.page_shift, c.max_pages - 1)];
+      if (page < 0 || page >= c.n_pages) continue;
+      const T* v = vc + (int64_t)page * c.page_stride + (int64_t)((kvh << c.page_shift) + (key & ((1 << c.page_shift) - 1))) * dh;
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const bool sees = keys_seen(mask[t], tree != nullptr, sq.len, key) & 1;
+#pragma unroll
+        for (int d = 0; d < NT; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int dim = BF ? d * 16 + kg * 4 + e : (d / 4) * 64 + kg * 16 + e * 4 + d % 4;
+            const float f = to_f32(v[min(dim, dh - 1)]);
+            o[t][d][e] += sees && (__float_as_uint(f) & 0x7f800000u) == 0x7f800000u ? f : 0.f;
+          }
+      }
+    }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     lsum[t] += __shfl_xor(lsum[t], 16, kWave);
@@ -601,7 +644,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
       for (int e = 0; e < 4; ++e) v4.v[e] = from_f32<T>(ref == -INFINITY ? 0.f : acc[e] * inv);
       *(Pack<T, 4>*)(out + (int64_t)(sq.row0 + i) * (H * dh) + (kvh * group + g) * dh + d) = v4;
     } else {
-      const int64_t at = ((int64_t)w * Hkv + kvh) * (blocks * BLOCK_ROWS) + qi;
+      const int64_t at = ((int64_t)w * Hkv + kvh) * (blocks * brows) + qi;
       *(f32x4*)(part + at * DH + d) = acc;
       if (d == 0) { pml[at * 2] = ref; pml[at * 2 + 1] = sum; }
     }
@@ -614,7 +657,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   if constexpr (SHARED) {
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const int qi = q0 + t * 16 + col;
+      const int qi = qtile(t) + col;
       if (qi < nq)
 #pragma unroll
         for (int x = 0; x < NT; ++x) store(qi, dim_of(x), dims(t, x), m2[t], lsum[t]);
@@ -702,32 +745,31 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, T* __restrict__ 
 
 // Shape of a launch, from what the host knows (the lengths are on the device).
 struct KvPlan {
-  int DH, QT, NW, blocks, slots, spare, prows;
+  int DH, QT, blocks, brows, slots, spare;
   bool shared;
   size_t part, pml, row_slot, total;         // workspace
 };
 
-inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max_keys, int H, int Hkv, int dh) {
+inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max_keys, int H, int Hkv, int dh, int target = 0) {
   KvPlan p;
   p.DH = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
   const int64_t nq = (int64_t)max_rows * (H / Hkv);
   p.QT = nq <= 16 ? 1 : nq <= 32 || p.DH == 128 || !bf ? 2 : 4;
-  p.NW = 4;
   p.shared = bf && nq > 16 * p.QT;
-  if (p.shared) {
-    p.QT = p.DH == 128 && nq <= 64 ? 1 : 2;
-    p.NW = nq <= 128 ? 4 : 8;
-  }
-  const int rows = 16 * p.QT * (p.shared ? p.NW : 1);
+  if (p.shared) p.QT = p.DH == 128 && nq <= 64 ? 1 : 2;
+  // rows of a block: no more than its waves hold, and evenly over the blocks
+  const int rows = 16 * p.QT * (p.shared ? KA_WAVES : 1);
   p.blocks = (int)((nq + rows - 1) / rows);
+  p.brows = (int)(((nq + p.blocks - 1) / p.blocks + 15) / 16 * 16);
   const int64_t steps = (max_keys + KA_STEP - 1) / KA_STEP;
-  int64_t spare = KA_TARGET / ((int64_t)Hkv * p.blocks);
+  // workgroups wanted: what the chip holds at once
+  const int resident = p.shared ? (p.DH == 64 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
+  int64_t spare = (target ? target : KA_CUS * resident) / ((int64_t)Hkv * p.blocks);
   if (spare > n_seqs * (steps - 1)) spare = n_seqs * (steps - 1);         // cuts that keys could be made at
   p.spare = (int)(spare < 0 ? 0 : spare);
   p.slots = n_seqs + p.spare;
-  p.prows = p.blocks * rows;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  const size_t all = p.spare ? (size_t)p.slots * Hkv * p.prows : 0;
+  const size_t all = p.spare ? (size_t)p.slots * Hkv * p.blocks * p.brows : 0;
   p.part = 0;
   p.pml = up(all * p.DH * 4);
   p.row_slot = p.pml + up(all * 8);
@@ -735,59 +777,60 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   return p;
 }
 
-template <typename T, int DH, int QT, int NW, bool SHARED, int S>
+inline int64_t kv_grid(const KvPlan& p, int Hkv) {
+  const int64_t pairs = (int64_t)p.slots * Hkv;
+  return p.blocks == 1 ? pairs : 8 * ((pairs + 7) / 8) * p.blocks;
+}
+
+template <typename T, int DH, int QT, bool SHARED, int S>
 hipError_t launch_kv_attention_as(const KvPlan& p, const void* q, const void* k, const void* v, const unsigned long long* tree, const KvView& c,
                                   void* out, char* ws, int H, int Hkv, int dh, int max_rows, hipStream_t st) {
   typedef KvTile<T, DH> L;
-  constexpr int ring = (SHARED ? 1 : NW) * S * 2 * L::BYTES, join = SHARED ? 0 : NW * 16 * QT * (DH + 2) * 4, lds = ring > join ? ring : join;
+  constexpr int ring = (SHARED ? 1 : KA_WAVES) * S * 2 * L::BYTES, join = SHARED ? 0 : KA_WAVES * 16 * QT * (DH + 2) * 4, lds = ring > join ? ring : join;
   static std::atomic<uint64_t> raised{0};
   if (lds > 65536) {
-    const hipError_t e = raise_lds_limit((const void*)kv_attention_kernel<T, DH, QT, NW, SHARED, S>, lds, raised);
+    const hipError_t e = raise_lds_limit((const void*)kv_attention_kernel<T, DH, QT, SHARED, S>, lds, raised);
     if (e != hipSuccess) return e;
   }
-  const int64_t grid = 8 * (((int64_t)p.slots * Hkv + 7) / 8) * p.blocks;
+  const unsigned grid = (unsigned)kv_grid(p, Hkv);
   float *part = (float*)(ws + p.part), *pml = (float*)(ws + p.pml);
   int4* row_slot = (int4*)(ws + p.row_slot);
-  kv_attention_kernel<T, DH, QT, NW, SHARED, S><<<(unsigned)grid, NW * 64, lds, st>>>(
-      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, part, pml, row_slot, H, Hkv, dh, max_rows, p.slots, p.spare, p.blocks,
+  kv_attention_kernel<T, DH, QT, SHARED, S><<<grid, KA_WAVES * 64, lds, st>>>(
+      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, part, pml, row_slot, H, Hkv, H / Hkv, dh, max_rows, p.slots, p.spare, p.blocks, p.brows,
       1.4426950408889634f / sqrtf((float)dh));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.spare) return e;
-  kv_join_kernel<T, DH><<<(unsigned)(((int64_t)c.n_rows * H + 3) / 4), 256, 0, st>>>(c, (T*)out, part, pml, row_slot, H, Hkv, dh, max_rows, p.slots, p.prows);
+  kv_join_kernel<T, DH><<<(unsigned)(((int64_t)c.n_rows * H + 3) / 4), 256, 0, st>>>(c, (T*)out, part, pml, row_slot, H, Hkv, dh, max_rows, p.slots, p.blocks * p.brows);
   return hipGetLastError();
 }
 
 inline hipError_t launch_kv_attention(bool bf, const KvPlan& p, const void* q, const void* k, const void* v, const unsigned long long* tree,
                                       const KvView& c, void* out, char* ws, int H, int Hkv, int dh, int max_rows, hipStream_t st) {
-#define ARMT_KA(T, D, Q, N, SH, S) return launch_kv_attention_as<T, D, Q, N, SH, S>(p, q, k, v, tree, c, out, ws, H, Hkv, dh, max_rows, st)
+#define ARMT_KA(T, D, Q, SH, S) return launch_kv_attention_as<T, D, Q, SH, S>(p, q, k, v, tree, c, out, ws, H, Hkv, dh, max_rows, st)
   if (bf && p.shared) {
-    if (p.DH == 64) {
-      if (p.NW == 4) ARMT_KA(bf16, 64, 2, 4, true, 4);
-      ARMT_KA(bf16, 64, 2, 8, true, 4);
-    }
-    if (p.QT == 1) ARMT_KA(bf16, 128, 1, 4, true, 4);
-    if (p.NW == 4) ARMT_KA(bf16, 128, 2, 4, true, 4);
-    ARMT_KA(bf16, 128, 2, 8, true, 4);
+    if (p.DH == 64) ARMT_KA(bf16, 64, 2, true, 4);
+    if (p.QT == 1) ARMT_KA(bf16, 128, 1, true, 4);
+    ARMT_KA(bf16, 128, 2, true, 4);
   }
   if (bf) {
     if (p.DH == 64) {
-      if (p.QT == 1) ARMT_KA(bf16, 64, 1, 4, false, 2);
-      if (p.QT == 2) ARMT_KA(bf16, 64, 2, 4, false, 2);
-      ARMT_KA(bf16, 64, 4, 4, false, 2);
+      if (p.QT == 1) ARMT_KA(bf16, 64, 1, false, 2);
+      if (p.QT == 2) ARMT_KA(bf16, 64, 2, false, 2);
+      ARMT_KA(bf16, 64, 4, false, 2);
     }
-    if (p.QT == 1) ARMT_KA(bf16, 128, 1, 4, false, 2);
-    ARMT_KA(bf16, 128, 2, 4, false, 2);
+    if (p.QT == 1) ARMT_KA(bf16, 128, 1, false, 2);
+    ARMT_KA(bf16, 128, 2, false, 2);
   }
   if (p.DH == 32) {
-    if (p.QT == 1) ARMT_KA(float, 32, 1, 4, false, 2);
-    ARMT_KA(float, 32, 2, 4, false, 2);
+    if (p.QT == 1) ARMT_KA(float, 32, 1, false, 2);
+    ARMT_KA(float, 32, 2, false, 2);
   }
   if (p.DH == 64) {
-    if (p.QT == 1) ARMT_KA(float, 64, 1, 4, false, 2);
-    ARMT_KA(float, 64, 2, 4, false, 2);
+    if (p.QT == 1) ARMT_KA(float, 64, 1, false, 2);
+    ARMT_KA(float, 64, 2, false, 2);
   }
-  if (p.QT == 1) ARMT_KA(float, 128, 1, 4, false, 2);
-  ARMT_KA(float, 128, 2, 4, false, 2);
+  if (p.QT == 1) ARMT_KA(float, 128, 1, false, 2);
+  ARMT_KA(float, 128, 2, false, 2);
 #undef ARMT_KA
 }
 
