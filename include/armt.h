@@ -374,7 +374,7 @@ armt_status armt_kv_attention(const armt_config *cfg, const armt_kv_cache *cache
  * out_parents (beam), out_tokens [n_seqs, n_out].  A logit of -inf bans a token, a score of -inf a beam (the first step has one live
  * beam): such continuations come last, with score -inf.  NaN logits count as -inf, +inf as the largest finite number; a score
  * that is not finite counts as -inf, and so do all of a beam without a logit above -inf.
- * Supported: n_out <= 64, n_beams * vocab < 2^31. */
+ * Supported: n_out <= 64, n_beams <= 64, n_beams * vocab <= 2^31 - 2^16, n_seqs * n_beams < 2^24. */
 size_t armt_beam_select_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out);
 armt_status armt_beam_select(const float *logits, int64_t ld_logits, const float *scores, int32_t n_seqs, int32_t n_beams, int32_t vocab,
                              int32_t n_out, float *out_scores, int32_t *out_parents, int32_t *out_tokens,

@@ -7,24 +7,28 @@ namespace armt {
 
 // ------------------------------------------------------------------------------------------------ selection
 // score(b, v) = scores[b] + x[b][v] - log sum_v' exp(x[b][v']); the n_out best of a sequence's beams x vocab, ties to the lowest b vocab + v.
-// First launch: every workgroup reads its part of one row of logits once, its four waves a quarter each; lanes keep a running maximum and sum,
-// and the wave the n_out best of what it has seen, sorted over its lanes (lane i: the i-th), so that a new value costs one comparison unless it
-// belongs among them.  Second launch: one workgroup per sequence joins the parts.  Reading the logits once bounds the large cases;
-// the small ones are two launches' latency.
+// First launch: a wave holds its part of one row of logits in registers, all loads in flight at once, takes their maximum and sum, and keeps those that
+// reach the n_out-th largest of its lanes' maxima: a bound of the n_out-th best that lets little more than n_out through.  The workgroup's survivors
+// are ranked by counting, and its n_out best written in order.  Second launch: one workgroup per sequence, the same over the parts' lists.
+// Reading the logits once bounds the large cases; the small ones are two launches' latency.
 //
 // Inside a row the order of the scores is that of the logits, so the lists hold 64-bit keys: the logit in an order-preserving form above the complement
 // of its index.  Scores of different rows are compared in 64 bits; the sums are of fp32 exponentials (random errors of 2^-24 each), added in fp32 per lane and in 64
 // bits across lanes.
 constexpr int BS_MAX = 64;             // n_out: a list lies over the lanes of one wave
+constexpr int BS_BEAMS = 64;           // beams of a sequence
 constexpr int BS_WAVES = 4;
-constexpr int BS_E = 8;                // logits per lane and step
+constexpr int BS_CAP = 256;            // survivors a wave may have; with more (ties, mostly) it sorts by insertion
+constexpr int BS_PICK = 8;             // waves of the second launch
 
 struct BeamPart { double sum; float top; int pad; };      // of one workgroup's part of a row: sum of exp(x - top)
 
-// A logit as it is taken: no NaN (the lowest), no +inf (the largest finite number), no -0.
-__device__ __forceinline__ float beam_logit(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e+38f) + 0.f; }
+constexpr float BS_MOST = 3.402823466e+38f;
+
+// A logit as it is taken: no NaN (the lowest), no +inf (the largest finite number).
+__device__ __forceinline__ float beam_logit(float x) { return x > -INFINITY ? fminf(x, BS_MOST) : -INFINITY; }
 __device__ __forceinline__ unsigned beam_order(float x) {
-  const unsigned u = __float_as_uint(x);
+  const unsigned u = __float_as_uint(x + 0.f);       // one zero
   return u ^ ((u & 0x80000000u) ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float beam_value(unsigned o) { return __uint_as_float(o ^ ((o & 0x80000000u) ? 0x80000000u : 0xffffffffu)); }
@@ -49,102 +53,142 @@ struct KeyList {
   }
 };
 
-// grid: rows x parts, block: 256.  list: [rows][parts][n_out], info: [rows][parts].
-__global__ __launch_bounds__(BS_WAVES * 64) void beam_scan_kernel(const float* __restrict__ logits, int64_t ld, int vocab, int n_out, int parts,
-                                                                   int per_wave, u64* __restrict__ list, BeamPart* __restrict__ info) {
+// The n-th largest of the lanes' values, or a little less: its leading BITS bits.
+template <int BITS>
+__device__ __forceinline__ unsigned nth_of_lanes(unsigned v, int n) {
+  unsigned low = 0;
+#pragma unroll
+  for (int b = 31; b >= 32 - BITS; --b) {
+    const unsigned mid = low | (1u << b);
+    low = __popcll(__ballot(v >= mid)) >= n ? mid : low;
+  }
+  return low;
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// grid: rows x parts, block: 256; a part is 4 x 64 E logits.  list: [sequences][n_out][beams][parts], info: [rows][parts].
+template <int E>
+__global__ __launch_bounds__(BS_WAVES * 64) __attribute__((amdgpu_waves_per_eu(E == 64 ? 5 : 1))) void beam_scan_kernel(const float* __restrict__ logits, int64_t ld, int beams, int vocab, int n_out, int parts,
+                                                                   u64* __restrict__ list, BeamPart* __restrict__ info) {
   struct alignas(4) Four { float v[4]; };
-  __shared__ u64 keys[BS_WAVES * BS_MAX];
-  __shared__ float tops[BS_WAVES];
+  __shared__ __align__(16) u64 keys[BS_WAVES][BS_CAP + 4];
+  __shared__ int counts[BS_WAVES];
+  __shared__ float tops[BS_WAVES], edges[BS_WAVES];
   __shared__ double sums[BS_WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x / parts, part = blockIdx.x - row * parts;
   const float* x = logits + (int64_t)row * ld;
-  const int64_t lo = min((int64_t)(part * BS_WAVES + wave) * per_wave, (int64_t)vocab), hi = min(lo + per_wave, (int64_t)vocab);
+  const int at = (int)min((int64_t)(part * BS_WAVES + wave) * (64 * E), (int64_t)vocab);
   constexpr float LOG2E = 1.4426950408889634f;
-  float top = -3.402823466e+38f, sum = 0.f, edge = -INFINITY;      // edge, edge_key: what a value has to reach to be among the best
-  u64 edge_key = 0;
-  KeyList best{0};
-  for (int64_t at = lo; at < hi; at += 64 * BS_E) {
-    float v[BS_E];
-    if (at + 64 * BS_E <= hi) {
+  // value e of a lane: index at + 256 (e / 4) + 4 lane + e % 4
+  float v[E];
 #pragma unroll
-      for (int g = 0; g < BS_E / 4; ++g) {
-        const Four f = *(const Four*)(x + at + g * 256 + lane * 4);
+  for (int g = 0; g < E / 4; ++g) {
+    if (at + (int64_t)g * 256 + 256 <= vocab) {
+      const Four f = *(const Four*)(x + at + g * 256 + lane * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[g * 4 + e] = f.v[e];
-      }
+      for (int e = 0; e < 4; ++e) v[g * 4 + e] = f.v[e];
     } else {
 #pragma unroll
-      for (int g = 0; g < BS_E / 4; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int64_t i = at + g * 256 + lane * 4 + e;
-          v[g * 4 + e] = i < hi ? x[i] : -INFINITY;
-        }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < BS_E; ++e) {
-      v[e] = beam_logit(v[e]);
-      mx = fmaxf(mx, v[e]);
-    }
-    const float t = fmaxf(top, mx);
-    sum *= __builtin_amdgcn_exp2f((top - t) * LOG2E);
-#pragma unroll
-    for (int e = 0; e < BS_E; ++e) sum += __builtin_amdgcn_exp2f((v[e] - t) * LOG2E);
-    top = t;
-    const u64 near = __ballot(mx >= edge);
-    if (__popcll(near) >= n_out) {       // many at once, as in the first step: a value that n_out lanes' maxima reach bounds the n_out-th best from below
-      const unsigned o = beam_order(mx);
-      unsigned low = 0;
-      for (int b = 31; b >= 12; --b) {
-        const unsigned mid = low | (1u << b);
-        if (__popcll(__ballot(o >= mid)) >= n_out) low = mid;
-      }
-      if (low > beam_order(-INFINITY)) edge = fmaxf(edge, beam_value(low));
-    }
-    if (near) {
-#pragma unroll
-      for (int e = 0; e < BS_E; ++e) {
-        const int64_t i = at + (e / 4) * 256 + lane * 4 + e % 4;
-        const u64 key = i < hi ? beam_key(v[e], (int)i) : 0;
-        u64 in = __ballot(v[e] >= edge && key > edge_key);
-        while (in) {
-          const u64 k = read_lane(key, __ffsll(in) - 1);
-          best.insert(k);
-          in &= in - 1;
-          const u64 last = read_lane(best.key, n_out - 1);
-          if (last) {
-            edge_key = last;
-            edge = beam_value((unsigned)(last >> 32));
-            in &= __ballot(key > last);
-          }
-        }
+      for (int e = 0; e < 4; ++e) {
+        const int64_t i = at + (int64_t)g * 256 + lane * 4 + e;
+        v[g * 4 + e] = i < vocab ? x[i] : -INFINITY;
       }
     }
   }
-  // ---- the wave's sum against its maximum, the workgroup's list: a key's rank is the number of larger ones
-  const float wtop = wave_max(top);
-  double s = (double)sum * exp((double)top - (double)wtop);
+  float mx = -INFINITY;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
-  if (lane == 0) { tops[wave] = wtop; sums[wave] = s; }
-  if (lane < n_out) keys[wave * n_out + lane] = best.key;
+  for (int e = 0; e < E; ++e) {
+    v[e] = beam_logit(v[e]);
+    mx = fmaxf(mx, v[e]);
+  }
+  // sum of exp(v - top) as exp2(v log2(e) - t2) with one rounding inside; what t2 is off by comes out of the sum again
+  const float top = fmaxf(wave_max(mx), -BS_MOST), t2 = top * LOG2E;
+  float sum = 0.f;
+  double off = 0.0;
+  if (fabsf(top) < 1e38f) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f(fmaf(v[e], LOG2E, -t2));
+    off = -(double)fmaf(top, LOG2E, -t2);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f((v[e] - top) * LOG2E);
+  }
+  const double wsum = wave_sum((double)sum) * exp2(off);
+  // a value that n_out lanes' maxima reach is not above the n_out-th best, of the row neither: the highest of the waves' serves all
+  const unsigned low = nth_of_lanes<20>(beam_order(mx), n_out);
+  if (lane == 0) edges[wave] = low > beam_order(-INFINITY) ? beam_value(low) : -INFINITY;
   __syncthreads();
-  const int n = BS_WAVES * n_out;
-  u64* dst = list + (int64_t)blockIdx.x * n_out;
-  if (threadIdx.x < n) {
-    const u64 mine = keys[threadIdx.x];
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += keys[i] > mine || (keys[i] == mine && i < (int)threadIdx.x);      // equal keys: nothing (0)
-    if (rank < n_out) dst[rank] = mine;
+  float edge = edges[0];
+#pragma unroll
+  for (int w = 1; w < BS_WAVES; ++w) edge = fmaxf(edge, edges[w]);
+  int have = 0;
+  auto index = [&](int e) __attribute__((always_inline)) { return at + (e / 4) * 256 + lane * 4 + e % 4; };
+  auto collect = [&](int e, u64 in) __attribute__((always_inline)) {
+    const int place = have + __popcll(in & ((1ull << lane) - 1));
+    if (((in >> lane) & 1) && place < BS_CAP) keys[wave][place] = beam_key(v[e], index(e));
+    have += __popcll(in);
+  };
+  if (edge > -INFINITY) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const u64 in = __ballot(v[e] >= edge);
+      if (in) collect(e, in);
+    }
+  } else {                               // (few logits, or hardly any above -inf)
+#pragma unroll
+    for (int e = 0; e < E; ++e) collect(e, __ballot(index(e) < vocab));
   }
+  if (have > BS_CAP) {
+    KeyList best{0};
+    u64 last = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const u64 key = index(e) < vocab ? beam_key(v[e], index(e)) : 0;
+      for (u64 in = __ballot(key > last); in; in &= __ballot(key > last)) {
+        best.insert(read_lane(key, __ffsll(in) - 1));
+        in &= in - 1;
+        last = read_lane(best.key, n_out - 1);
+      }
+    }
+    if (lane < n_out) keys[wave][lane] = best.key;       // (all of them: more than BS_CAP were there)
+    have = n_out;
+  }
+  if (lane < 4) keys[wave][have + lane] = 0;             // read four at a time
+  if (lane == 0) { counts[wave] = have; tops[wave] = top; sums[wave] = wsum; }
+  __syncthreads();
+  // ---- the workgroup's list: a key's place is the number of larger ones
+  const int seq = row / beams, lists = beams * parts;
+  u64* dst = list + (int64_t)seq * n_out * lists + (row - seq * beams) * parts + part;
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < BS_WAVES; ++w) all += counts[w];
+  for (int i = lane; i < have; i += 64) {
+    const u64 mine = keys[wave][i];
+    int rank = 0;
+#pragma unroll
+    for (int w = 0; w < BS_WAVES; ++w) {
+      const int n = counts[w];
+#pragma unroll 2
+      for (int j = 0; j < n; j += 4) {
+        const ulonglong2 p = *(const ulonglong2*)&keys[w][j], q = *(const ulonglong2*)&keys[w][j + 2];
+        rank += (p.x > mine) + (p.y > mine) + (q.x > mine) + (q.y > mine);
+      }
+    }
+    if (rank < n_out) dst[(int64_t)rank * lists] = mine;
+  }
+  for (int i = all + (int)threadIdx.x; i < n_out; i += BS_WAVES * 64) dst[(int64_t)i * lists] = 0;
   if (threadIdx.x == 0) {
     float t = tops[0];
     for (int i = 1; i < BS_WAVES; ++i) t = fmaxf(t, tops[i]);
-    double all = 0.0;
-    for (int i = 0; i < BS_WAVES; ++i) all += sums[i] * exp((double)tops[i] - (double)t);
-    info[blockIdx.x] = BeamPart{all, t, 0};
+    double total = 0.0;
+    for (int i = 0; i < BS_WAVES; ++i) total += sums[i] * exp((double)tops[i] - (double)t);
+    info[blockIdx.x] = BeamPart{total, t, 0};
   }
 }
 
@@ -169,95 +213,200 @@ struct ScoreList {
   }
 };
 
-// grid: sequences, block: 256.  Wave w joins rows w, w + 4, ... of its sequence; the rows' lists then meet in wave 0.
-__global__ __launch_bounds__(BS_WAVES * 64) void beam_pick_kernel(const u64* __restrict__ list, const BeamPart* __restrict__ info, const float* __restrict__ scores,
-                                                                   int beams, int vocab, int n_out, int parts, float* __restrict__ out_scores,
-                                                                   int32_t* __restrict__ out_parents, int32_t* __restrict__ out_tokens) {
-  __shared__ u64 sc[BS_WAVES * BS_MAX];
-  __shared__ unsigned ix[BS_WAVES * BS_MAX];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), seq = blockIdx.x;
-  ScoreList mine{0, 0xffffffffu};
-  for (int b = wave; b < beams; b += BS_WAVES) {
-    const int64_t row = (int64_t)seq * beams + b;
-    const BeamPart* pi = info + row * parts;
-    const u64* pl = list + row * parts * n_out;
-    float top = -3.402823466e+38f;
-    for (int i = lane; i < parts; i += 64) top = fmaxf(top, pi[i].top);
-    top = wave_max(top);
-    double sum = 0.0;
-    for (int i = lane; i < parts; i += 64) sum += pi[i].sum * exp((double)pi[i].top - (double)top);
+// grid: sequences, block: 512.
+__global__ __launch_bounds__(BS_PICK * 64) void beam_pick_kernel(const u64* __restrict__ list, const BeamPart* __restrict__ info, const float* __restrict__ scores,
+                                                                  int beams, int vocab, int n_out, int parts, float* __restrict__ out_scores,
+                                                                  int32_t* __restrict__ out_parents, int32_t* __restrict__ out_tokens) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int CAP = BS_CAP + 4;
+  u64* sc = (u64*)smem;                                     // [waves][CAP]
+  unsigned* ix = (unsigned*)(sc + BS_PICK * CAP);           // the same
+  int* counts = (int*)(ix + BS_PICK * CAP);                 // [waves], padded to 16
+  double* shift = (double*)(counts + 16);                   // [beams] log of the sum
+  double* top = shift + beams;                              // [beams] +inf: no continuation of the beam has a score
+  double* before = top + beams;                             // [beams]
+  const int fin = (BS_PICK * CAP * 12 + 64 + beams * 24 + 15) & ~15;        // the last list: as sc and ix
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), seq = blockIdx.x, lists = beams * parts;
+  const int64_t row0 = (int64_t)seq * beams;
+  const u64* pl = list + (int64_t)seq * n_out * lists;
+  const int n = n_out * lists;                              // (host: below 2^31)
+  constexpr int EARLY = 8, STEP = BS_PICK * 64;
+  u64 early[EARLY];                                         // the first candidates' keys are on their way while the sums are made
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-    const float before = scores[row];
-    const bool dead = !(before > -INFINITY && before < INFINITY) || !(sum > 0.0);       // no continuation of it has a score: its candidates are -inf, by index
-    const double shift = log(sum);
-    // the row's own best, by key
-    KeyList best{0};
-    if (!dead) {
-      u64 edge = 0;
-      for (int i0 = 0; i0 < parts * n_out; i0 += 64) {
-        const u64 k = i0 + lane < parts * n_out ? pl[i0 + lane] : 0;
-        u64 in = __ballot(k > edge);
-        while (in) {
-          best.insert(read_lane(k, __ffsll(in) - 1));
-          edge = read_lane(best.key, n_out - 1);
-          in &= in - 1;
-          in &= __ballot(k > edge);
-        }
+  for (int k = 0; k < EARLY; ++k) early[k] = k * STEP + (int)threadIdx.x < n ? pl[k * STEP + threadIdx.x] : 0;
+  for (int b = wave; b < beams; b += BS_PICK) {
+    const BeamPart* pi = info + (row0 + b) * parts;
+    const float score = scores[row0 + b];
+    float t = -3.402823466e+38f;
+    for (int i = lane; i < parts; i += 64) t = fmaxf(t, pi[i].top);
+    t = wave_max(t);
+    double sum = 0.0;
+    for (int i = lane; i < parts; i += 64) sum += pi[i].sum * exp((double)pi[i].top - (double)t);
+    sum = wave_sum(sum);
+    const bool dead = !(score > -INFINITY && score < INFINITY) || !(sum > 0.0);
+    if (lane == 0) { shift[b] = log(sum); top[b] = dead ? INFINITY : (double)t; before[b] = score; }
+  }
+  __syncthreads();
+  // candidate i: entry i / lists of list i % lists, so that neighbouring lanes have the same entry of different lists and their maxima are alike.
+  // Score and flat index; 0: none.  A beam without a score offers its first tokens, at -inf.
+  const float per_list = 1.f / (float)lists, per_part = 1.f / (float)parts;
+  auto quotient = [](int x, int d, float inv) __attribute__((always_inline)) {      // off by little: put right
+    int q = (int)((float)x * inv);
+    while (x < q * d) --q;
+    while (x - q * d >= d) ++q;
+    return q;
+  };
+  auto candidate = [&](int i, u64 key, u64& s, unsigned& at) __attribute__((always_inline)) {
+    const int j = quotient(i, lists, per_list), l = i - j * lists, b = quotient(l, parts, per_part);
+    const bool dead = top[b] == INFINITY;
+    const unsigned token = dead ? (unsigned)j : ~(unsigned)key;
+    const double value = dead ? -INFINITY : before[b] + (((double)beam_value((unsigned)(key >> 32)) - top[b]) - shift[b]);
+    s = i < n && (dead ? l == b * parts && j < vocab : key != 0) ? score_order(value) : 0;
+    at = (unsigned)b * (unsigned)vocab + token;
+  };
+  unsigned mx = 0, at_early[EARLY];
+#pragma unroll
+  for (int k = 0; k < EARLY; ++k) {
+    candidate(min(k * STEP + (int)threadIdx.x, n), early[k], early[k], at_early[k]);
+    mx = max(mx, (unsigned)(early[k] >> 32));
+  }
+  for (int i = EARLY * STEP + (int)threadIdx.x; i < n; i += STEP) {
+    u64 s;
+    unsigned at;
+    candidate(i, pl[i], s, at);
+    mx = max(mx, (unsigned)(s >> 32));
+  }
+  const unsigned low = nth_of_lanes<32>(mx, n_out);
+  if (lane == 0) counts[wave] = (int)low;
+  __syncthreads();
+  unsigned edge = 1;                                        // (a score's upper word is never 0)
+  for (int w = 0; w < BS_PICK; ++w) edge = max(edge, (unsigned)counts[w]);
+  __syncthreads();
+  int have = 0;
+  auto collect = [&](u64 s, unsigned at) __attribute__((always_inline)) {
+    const u64 in = __ballot((unsigned)(s >> 32) >= edge);
+    const int place = have + __popcll(in & ((1ull << lane) - 1));
+    if (((in >> lane) & 1) && place < BS_CAP) {
+      sc[wave * CAP + place] = s;
+      ix[wave * CAP + place] = at;
+    }
+    have += __popcll(in);
+  };
+#pragma unroll
+  for (int k = 0; k < EARLY; ++k) collect(early[k], at_early[k]);
+  for (int i0 = EARLY * STEP + wave * 64; i0 < n; i0 += STEP) {
+    u64 s = 0;
+    unsigned at = 0;
+    if (i0 + lane < n) candidate(i0 + lane, pl[i0 + lane], s, at);
+    collect(s, at);
+  }
+  const bool many = have > BS_CAP;
+  if (many) {
+    ScoreList best{0, 0xffffffffu};
+    for (int i0 = wave * 64; i0 < n; i0 += BS_PICK * 64) {
+      u64 s = 0;
+      unsigned at = 0xffffffffu;
+      if (i0 + lane < n) candidate(i0 + lane, pl[i0 + lane], s, at);
+      auto better = [&]() __attribute__((always_inline)) {
+        return __ballot(s != 0 && ScoreList::before(s, at, read_lane(best.score, n_out - 1), read_lane(best.at, n_out - 1)));
+      };
+      for (u64 in = better(); in; in &= better()) {
+        const int l = __ffsll(in) - 1;
+        best.insert(read_lane(s, l), read_lane(at, l));
+        in &= in - 1;
       }
     }
-    const bool have = dead ? lane < min(n_out, vocab) : lane < n_out && best.key != 0;
-    const unsigned token = dead ? (unsigned)lane : ~(unsigned)best.key;
-    const double value = dead ? -INFINITY : (double)before + (((double)beam_value((unsigned)(best.key >> 32)) - (double)top) - shift);
-    const u64 s = have ? score_order(value) : 0;
-    const unsigned at = (unsigned)b * (unsigned)vocab + token;
-    // they come in falling order: stop at the first that is not among the wave's best
-    for (int l = 0; l < n_out; ++l) {
-      const u64 cs = read_lane(s, l);
-      const unsigned ca = read_lane(at, l);
-      if (cs == 0 || !ScoreList::before(cs, ca, read_lane(mine.score, n_out - 1), read_lane(mine.at, n_out - 1))) break;
-      mine.insert(cs, ca);
+    if (lane < n_out) { sc[wave * CAP + lane] = best.score; ix[wave * CAP + lane] = best.at; }
+    have = n_out;
+  }
+  if (lane == 0) counts[wave] = have;
+  if (threadIdx.x == 0) counts[BS_PICK] = 0;
+  __syncthreads();
+  int all = 0;
+  for (int w = 0; w < BS_PICK; ++w) all += counts[w];
+  if (all > 2 * 64) {                                       // few lanes had most of them: the same once more, among these
+    unsigned m = 0;
+    for (int i = lane; i < have; i += 64) m = max(m, (unsigned)(sc[wave * CAP + i] >> 32));
+    const unsigned l2 = nth_of_lanes<32>(m, n_out);
+    __syncthreads();
+    if (lane == 0) counts[wave] = (int)l2;
+    __syncthreads();
+    for (int w = 0; w < BS_PICK; ++w) edge = max(edge, (unsigned)counts[w]);
+  }
+  // side by side, in any order: a score's place is the number of better ones
+  u64* fs = (u64*)(smem + fin);
+  unsigned* fi = (unsigned*)(fs + BS_PICK * CAP);
+  for (int i0 = 0; i0 < have; i0 += 64) {
+    const int i = i0 + lane;
+    const u64 s = i < have ? sc[wave * CAP + i] : 0;
+    const u64 in = __ballot(s != 0 && (unsigned)(s >> 32) >= edge);
+    int base = 0;
+    if (lane == 0 && in) base = atomicAdd(&counts[BS_PICK], __popcll(in));
+    base = __builtin_amdgcn_readfirstlane(base);
+    if ((in >> lane) & 1) {
+      const int place = base + __popcll(in & ((1ull << lane) - 1));
+      fs[place] = s;
+      fi[place] = ix[wave * CAP + i];
     }
   }
-  if (lane < n_out) { sc[wave * n_out + lane] = mine.score; ix[wave * n_out + lane] = mine.at; }
   __syncthreads();
-  const int n = BS_WAVES * n_out;
-  if (threadIdx.x >= n) return;
-  const u64 s = sc[threadIdx.x];
-  const unsigned a = ix[threadIdx.x];
-  int rank = 0;
-  for (int i = 0; i < n; ++i) rank += ScoreList::before(sc[i], ix[i], s, a) || (sc[i] == s && ix[i] == a && i < (int)threadIdx.x);
-  if (rank < n_out && s != 0) {
-    const int64_t o = (int64_t)seq * n_out + rank;
-    out_scores[o] = (float)score_value(s);
-    out_parents[o] = (int32_t)(a / (unsigned)vocab);
-    out_tokens[o] = (int32_t)(a % (unsigned)vocab);
+  const int m = counts[BS_PICK];
+  if (threadIdx.x < 4) fs[m + threadIdx.x] = 0;             // read four at a time; 0 is behind every score
+  __syncthreads();
+  for (int i = threadIdx.x; i < m; i += STEP) {
+    const u64 s = fs[i];
+    const unsigned at = fi[i];
+    int rank = 0;
+#pragma unroll 2
+    for (int j = 0; j < m; j += 4) {
+      const ulonglong2 p = *(const ulonglong2*)&fs[j], q = *(const ulonglong2*)&fs[j + 2];
+      const uint4 x = *(const uint4*)&fi[j];
+      rank += ScoreList::before(p.x, x.x, s, at) + ScoreList::before(p.y, x.y, s, at) + ScoreList::before(q.x, x.z, s, at) +
+              ScoreList::before(q.y, x.w, s, at);
+    }
+    if (rank < n_out) {
+      const int64_t o = (int64_t)seq * n_out + rank;
+      const unsigned beam = at / (unsigned)vocab;
+      out_scores[o] = (float)score_value(s);
+      out_parents[o] = (int32_t)beam;
+      out_tokens[o] = (int32_t)(at - beam * (unsigned)vocab);
+    }
   }
 }
 
-// Workgroups of a row: enough to fill the chip with few rows, at least one step of every wave each.
+// Logits per lane of the first launch: as many as leave a wave for most compute units, as fewer and longer lists serve the second launch (4 rows of 128256:
+// 8, 16, 32 logits 14.0, 12.4, 12.0 us; 192 rows of 100003: 16, 32, 64 logits 38.7, 32.4, 32.6).
+inline int beam_width(int64_t rows, int vocab) {
+  for (int e = 64; e > 8; e /= 2)
+    if (rows * ((vocab + 64 * e - 1) / (64 * e)) >= 200) return e;
+  return 8;
+}
 inline int beam_parts(int64_t rows, int vocab) {
-  const int64_t step = BS_WAVES * 64 * BS_E, most = (vocab + step - 1) / step, want = (1024 + rows - 1) / rows;
-  return (int)(want < most ? want : most);
+  const int part = BS_WAVES * 64 * beam_width(rows, vocab);
+  return (int)(((int64_t)vocab + part - 1) / part);
 }
 
 inline size_t beam_workspace(int64_t rows, int vocab, int n_out) {
-  const size_t lists = (size_t)rows * beam_parts(rows, vocab) * n_out * sizeof(u64);
-  return (lists + 255) / 256 * 256 + (size_t)rows * beam_parts(rows, vocab) * sizeof(BeamPart);
+  const size_t all = (size_t)rows * beam_parts(rows, vocab);
+  return (all * n_out * sizeof(u64) + 255) / 256 * 256 + all * sizeof(BeamPart);
 }
 
 inline hipError_t launch_beam_select(const float* logits, int64_t ld, const float* scores, int n_seqs, int beams, int vocab, int n_out, float* out_scores,
                                      int32_t* out_parents, int32_t* out_tokens, char* ws, hipStream_t st) {
   const int64_t rows = (int64_t)n_seqs * beams;
-  const int parts = beam_parts(rows, vocab);
-  const int64_t cut = (int64_t)parts * BS_WAVES;
-  const int per_wave = (int)((((int64_t)vocab + cut - 1) / cut + 3) / 4 * 4);
+  const int parts = beam_parts(rows, vocab), width = beam_width(rows, vocab);
   u64* list = (u64*)ws;
   BeamPart* info = (BeamPart*)(ws + ((size_t)rows * parts * n_out * sizeof(u64) + 255) / 256 * 256);
-  beam_scan_kernel<<<(unsigned)(rows * parts), BS_WAVES * 64, 0, st>>>(logits, ld, vocab, n_out, parts, per_wave, list, info);
+#define ARMT_BS(E) beam_scan_kernel<E><<<(unsigned)(rows * parts), BS_WAVES * 64, 0, st>>>(logits, ld, beams, vocab, n_out, parts, list, info)
+  if (width == 64) ARMT_BS(64);
+  else if (width == 32) ARMT_BS(32);
+  else if (width == 16) ARMT_BS(16);
+  else ARMT_BS(8);
+#undef ARMT_BS
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  beam_pick_kernel<<<n_seqs, BS_WAVES * 64, 0, st>>>(list, info, scores, beams, vocab, n_out, parts, out_scores, out_parents, out_tokens);
+  const int lists = BS_PICK * (BS_CAP + 4) * 12, lds = lists + ((64 + beams * 24 + 15) & ~15) + lists;      // under 64 KB for BS_BEAMS beams
+  beam_pick_kernel<<<n_seqs, BS_PICK * 64, lds, st>>>(list, info, scores, beams, vocab, n_out, parts, out_scores, out_parents, out_tokens);
   return hipGetLastError();
 }
 
@@ -273,22 +422,21 @@ struct BeamStates { BeamState s[BR_STATES]; int n; };
 typedef unsigned br16 __attribute__((ext_vector_type(4), aligned(4)));       // 16 and 8 bytes at any multiple of four
 typedef unsigned br8 __attribute__((ext_vector_type(2), aligned(4)));
 
+// Rows that a beam continues, by beam; a beam that stays where it is takes the row of one that does not, which is read anyway.
 template <int KMAX, typename U>
 __device__ __forceinline__ void reorder_column(const char* src, char* dst, int64_t src_stride, int64_t dst_stride, const int32_t* __restrict__ par, int beams,
-                                               bool in_place) {
+                                               bool in_place, int moved) {
   U v[KMAX];
 #pragma unroll
-  for (int k = 0; k < KMAX; ++k)
-    if (k < beams) {
-      const int p = min(max(par[k], 0), beams - 1);
-      if (!(in_place && p == k)) v[k] = *(const U*)(src + p * src_stride);
-    }
+  for (int k = 0; k < KMAX; ++k) {
+    const int j = min(k, beams - 1), p = min(max(par[j], 0), beams - 1);
+    v[k] = *(const U*)(src + (in_place && p == j ? moved : p) * src_stride);
+  }
 #pragma unroll
-  for (int k = 0; k < KMAX; ++k)
-    if (k < beams) {
-      const int p = min(max(par[k], 0), beams - 1);
-      if (!(in_place && p == k)) *(U*)(dst + k * dst_stride) = v[k];
-    }
+  for (int k = 0; k < KMAX; ++k) {
+    const int p = k < beams ? min(max(par[k], 0), beams - 1) : k;
+    if (k < beams && !(in_place && p == k)) *(U*)(dst + k * dst_stride) = v[k];
+  }
 }
 
 // grid: all states' blocks (a sequence's columns side by side), block: 256.
@@ -301,12 +449,18 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(BeamStates st, const 
   const int64_t col = ((int64_t)(b - seq * t.cols) * 256 + threadIdx.x) * (int64_t)sizeof(U);
   const int32_t* par = parents + (int64_t)seq * beams;
   const bool in_place = t.src == t.dst;
+  int moved = -1;
+  for (int k = 0; k < beams; ++k) {
+    const int p = min(max(par[k], 0), beams - 1);
+    if (!in_place || p != k) moved = p;
+  }
+  if (moved < 0) return;
   const char* src = t.src + (int64_t)seq * beams * t.src_stride + col;
   char* dst = t.dst + (int64_t)seq * beams * t.dst_stride + col;
-  if (col + (int64_t)sizeof(U) <= t.row_bytes) reorder_column<KMAX, U>(src, dst, t.src_stride, t.dst_stride, par, beams, in_place);
+  if (col + (int64_t)sizeof(U) <= t.row_bytes) reorder_column<KMAX, U>(src, dst, t.src_stride, t.dst_stride, par, beams, in_place, moved);
   else if constexpr (sizeof(U) > 4) {                // the last, shorter piece of a row
     for (int64_t x = 0; x < t.row_bytes - col; x += 4)
-      reorder_column<KMAX, unsigned>(src + x, dst + x, t.src_stride, t.dst_stride, par, beams, in_place);
+      reorder_column<KMAX, unsigned>(src + x, dst + x, t.src_stride, t.dst_stride, par, beams, in_place, moved);
   }
 }
 

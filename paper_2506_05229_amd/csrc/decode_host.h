@@ -81,8 +81,8 @@ armt_status armt_kv_attention(const armt_config* cfg, const armt_kv_cache* cache
 }
 
 size_t armt_beam_select_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out) {
-  if (n_seqs < 1 || n_beams < 1 || vocab < 1 || n_out < 1 || n_out > BS_MAX || (int64_t)n_beams * vocab < n_out ||
-      (int64_t)n_beams * vocab > 0x7fffffff || (int64_t)n_seqs * n_beams > 0xffffff)
+  if (n_seqs < 1 || n_beams < 1 || vocab < 1 || n_out < 1 || n_out > BS_MAX || n_beams > BS_BEAMS || (int64_t)n_beams * vocab < n_out ||
+      (int64_t)n_beams * vocab > 0x7fff0000 || (int64_t)n_seqs * n_beams > 0xffffff)
     return 0;
   return beam_workspace((int64_t)n_seqs * n_beams, vocab, n_out);
 }
@@ -102,7 +102,7 @@ armt_status armt_beam_select(const float* logits, int64_t ld_logits, const float
 armt_status armt_beam_reorder(const int32_t* parents, int32_t n_seqs, int32_t n_beams, const armt_beam_state* states, int32_t n_states, void* hip_stream) {
   if (!parents || !states) return ARMT_ERR_NULL;
   if (n_seqs < 1 || n_beams < 1 || n_states < 1) return ARMT_ERR_SHAPE;
-  if (n_beams > 64 || n_states > BR_STATES) return ARMT_ERR_UNSUPPORTED;
+  if (n_beams > BS_BEAMS || n_states > BR_STATES) return ARMT_ERR_UNSUPPORTED;
   BeamStates st{};
   const int64_t rows = (int64_t)n_seqs * n_beams;
   for (int i = 0; i < n_states; ++i) {

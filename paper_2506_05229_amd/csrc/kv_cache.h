@@ -23,17 +23,27 @@ struct KvView {
 // (j, j + dh/2) by p theta^(-2j/dh).  The angle is taken in turns and in double, and only its fraction is rounded to fp32: a position
 // of 10^9 loses nothing.  A block takes `per` rows: first where each of them goes and the cosines and sines of all of them, into LDS, then VEC pairs
 // at a time without another barrier; a thread's first loads are on their way before the first barrier.  Bytes bound it (each
-// element read and written once), for few rows the two loads that lead to a row's page.
+// element read and written once), for few rows the two loads that lead to a row's page.  Many rows are written past the L2, which a row's heads, a
+// page apart, would leave in pieces: 16000 rows of (32 + 2 x 8) x 64 bf16 60 -> 38 us (5.1 TB/s).
 // grid: ceil(n_rows / per), block: 256.
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
 
-constexpr int KV_ROWS = 4;               // most rows of a block
+constexpr int KV_ROWS = 2;               // most rows of a block
+constexpr int64_t KV_STREAM_BYTES = 16 << 20;      // what is written bypasses the L2 from here on (half of the L2s of the eight XCDs)
 
-template <typename T, int VEC>
+// STREAM: a store that does not stay in the L2.
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_pack(void* at, const V& v) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  if constexpr (STREAM && sizeof(V) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)at);
+  else *(V*)at = v;
+}
+
+template <typename T, int VEC, bool STREAM>
 __global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qkv, int64_t ld, KvView c, const int32_t* __restrict__ positions,
                                                         T* __restrict__ q_out, T* __restrict__ kc, T* __restrict__ vc,
-                                                        int H, int Hkv, int dh, int per, double log2_theta) {
+                                                        int H, int Hkv, int dh, int per, unsigned per_hv, unsigned per_dv, double log2_theta) {
   typedef Pack<T, VEC> V;
   __shared__ float cs[KV_ROWS][128];     // cos dh/2 | sin dh/2
   __shared__ int64_t at[KV_ROWS];        // element of the key in head 0 of its page; -1: no page; -2: nobody's row
@@ -41,23 +51,25 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qk
   const int half = dh >> 1, hv = half / VEC, rot_items = (H + Hkv) * hv, dv = dh / VEC, row_items = rot_items + Hkv * dv;
   const int tid = threadIdx.x, P = 1 << c.page_shift;
   const int64_t row0 = (int64_t)blockIdx.x * per;
-  const int rows = (int)min((int64_t)per, c.n_rows - row0), items = rows * row_items;
-  // item i: pair of VEC columns (j, j + half) of rotated head h, or VEC columns of a value head
-  auto place = [&](int i, int& r, int& h, int& j) __attribute__((always_inline)) {
-    r = i / row_items;
-    const int x = i - r * row_items;
-    if (x < rot_items) { h = x / hv; j = (x - h * hv) * VEC; }
-    else { h = (x - rot_items) / dv; j = (x - rot_items - h * dv) * VEC; h += H + Hkv; }
+  const int rows = (int)min((int64_t)per, c.n_rows - row0);
+  // A thread's items are 256 apart: x of row r, either a pair of VEC columns (j, j + half) of rotated head h or VEC columns of a value head
+  struct Item { V a, b; int r, x, h, j; };
+  auto load = [&](Item& it) __attribute__((always_inline)) {
+    while (it.x >= row_items) { it.x -= row_items; ++it.r; }
+    if (it.r >= rows) return;
+    if (it.x < rot_items) { it.h = hv == 1 ? it.x : (int)__umulhi(it.x, per_hv); it.j = (it.x - it.h * hv) * VEC; }
+    else { const int y = it.x - rot_items; it.h = __umulhi(y, per_dv); it.j = (y - it.h * dv) * VEC; it.h += H + Hkv; }
+    const T* src = qkv + (row0 + it.r) * ld + it.h * dh + it.j;
+    it.a = *(const V*)src;
+    if (it.h < H + Hkv) it.b = *(const V*)(src + half);
   };
-  V a, b;
-  int r1 = 0, h1 = 0, j1 = 0;            // place of the item whose values are in a, b
-  auto load = [&](int i) __attribute__((always_inline)) {
-    place(i, r1, h1, j1);
-    const T* src = qkv + (row0 + r1) * ld + h1 * dh + j1;
-    a = *(const V*)src;
-    if (h1 < H + Hkv) b = *(const V*)(src + half);
-  };
-  if (tid < items) load(tid);
+  Item next[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    next[n].r = 0;
+    next[n].x = n * 256 + tid;
+    load(next[n]);
+  }
   static_assert(KV_ROWS * 64 <= 256, "an angle per thread");
   const int ar = tid / half, aj = tid - ar * half, pos = positions && ar < rows ? positions[row0 + ar] : 0;
   if (tid < KV_ROWS) { at[tid] = -2; slot[tid] = 0; }
@@ -79,42 +91,49 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qk
     cs[ar][half + aj] = sinpif(f);
   }
   __syncthreads();
-  for (int i = tid; i < items;) {
-    const int r = r1, h = h1, j = j1;
+  while (next[0].r < rows) {
+    const Item it = next[0];
+    const int r = it.r, h = it.h, j = it.j;
     const int64_t to = at[r];
-    const V a0 = a, b0 = b;
-    i += 256;
-    if (i < items) load(i);
+    next[0] = next[1];
+    next[1].r = next[0].r;
+    next[1].x = next[0].x + 256;
+    load(next[1]);
     if (to == -2) continue;              // behind the last sequence: left as it is
     if (h < H + Hkv) {
       V x, y;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float co = cs[r][j + e], si = cs[r][half + j + e], u = to_f32(a0.v[e]), w = to_f32(b0.v[e]);
+        const float co = cs[r][j + e], si = cs[r][half + j + e], u = to_f32(it.a.v[e]), w = to_f32(it.b.v[e]);
         x.v[e] = from_f32<T>(u * co - w * si);
         y.v[e] = from_f32<T>(w * co + u * si);
       }
       T* dst = h < H ? q_out + (row0 + r) * (int64_t)(H * dh) + h * dh : kc + to + (int64_t)(h - H) * P * dh;
       if (h < H || to >= 0) {
-        *(V*)(dst + j) = x;
-        *(V*)(dst + half + j) = y;
+        store_pack<STREAM>(dst + j, x);
+        store_pack<STREAM>(dst + half + j, y);
       }
     } else if (to >= 0) {
-      *(V*)(vc + to + (int64_t)(h - H - Hkv) * P * dh + j) = a0;
+      store_pack<STREAM>(vc + to + (int64_t)(h - H - Hkv) * P * dh + j, it.a);
     }
   }
 }
 
 inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const KvView& c, const int32_t* positions, void* q_out,
                                    void* k, void* v, int H, int Hkv, int dh, double theta, hipStream_t st) {
-  int per = (c.n_rows + 2047) / 2048;                  // eight blocks per compute unit as long as a block takes no more than its rows
-  per = per > KV_ROWS ? KV_ROWS : per;
+  const int per = c.n_rows > 2048 ? KV_ROWS : 1;        // one row per block as long as the chip holds all blocks at once
   const unsigned grid = (unsigned)(((int64_t)c.n_rows + per - 1) / per);
   const double l2 = log2(theta);
-#define ARMT_KV(T, VEC) kv_append_kernel<T, VEC><<<grid, 256, 0, st>>>((const T*)qkv, ld, c, positions, (T*)q_out, (T*)k, (T*)v, H, Hkv, dh, per, l2)
-  if (bf) ARMT_KV(bf16, 8);
-  else if (dh % 8 == 0) ARMT_KV(float, 4);
-  else ARMT_KV(float, 2);
+  auto over = [](int d) { return (unsigned)(0xffffffffu / (unsigned)d + 1); };        // x / d = the high word of x over(d) while x d < 2^32 (d > 1)
+  const bool stream = (int64_t)c.n_rows * (H + 2 * Hkv) * dh * (bf ? 2 : 4) >= KV_STREAM_BYTES;
+#define ARMT_KV(T, VEC, STREAM)                                                                                                    \
+  kv_append_kernel<T, VEC, STREAM><<<grid, 256, 0, st>>>((const T*)qkv, ld, c, positions, (T*)q_out, (T*)k, (T*)v, H, Hkv, dh, per, \
+                                                         over(dh / 2 / VEC), over(dh / VEC), l2)
+  if (bf && stream) ARMT_KV(bf16, 8, true);
+  else if (bf) ARMT_KV(bf16, 8, false);
+  else if (dh % 8) ARMT_KV(float, 2, false);
+  else if (stream) ARMT_KV(float, 4, true);
+  else ARMT_KV(float, 4, false);
 #undef ARMT_KV
   return hipGetLastError();
 }
