@@ -487,14 +487,11 @@ class TokenEnds:
 
 
 # ---------------------------------------------------------------- decoding
-def _on(torch, device):
-    """Context in which `device` is the current one (the library launches on the current device)."""
-    import contextlib
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-
-def _raw_stream(torch, device):
-    return torch.cuda.current_stream(device).cuda_stream
+# These are called once per token and layer, so what surrounds the library call counts: integer device numbers and raw stream handles.
+def _on_device(torch, index, call, *args, **kw):
+    """call(...) with device `index` current: the library launches on the current device."""
+    with torch.cuda.device(index):
+        return call(*args, **kw)
 
 
 class KvCache:
@@ -519,60 +516,67 @@ class KvCache:
             assert tuple(t.shape[1:]) == (shape.n_kv_heads, self.page_len, shape.head_dim) and t[0].is_contiguous()
         assert k.shape[0] == 1 or k.stride(0) == v.stride(0)
         self.device = k.device
+        self._index = k.get_device()
         self._c = ArmtKvCache(k=k.data_ptr(), v=v.data_ptr(), n_pages=k.shape[0], page_len=self.page_len, page_stride=k.stride(0) if k.shape[0] > 1 else 0)
         self._cfg_ref = C.byref(self.cfg)
 
     def _call(self, pages, lens, row_start):
         """The armt_kv_cache of one call (its own, so that threads may share the cache)."""
-        c, n = ArmtKvCache.from_buffer_copy(self._c), lens.shape[0]
-        i32 = self.torch.int32
-        assert pages.dtype == i32 and lens.dtype == i32 and row_start.dtype == i32
-        assert pages.device == self.device and lens.device == self.device and row_start.device == self.device
-        assert pages.shape[0] == n and row_start.shape[0] == n + 1 and pages.is_contiguous() and lens.is_contiguous() and row_start.is_contiguous()
-        c.pages, c.lens, c.row_start = pages.data_ptr(), lens.data_ptr(), row_start.data_ptr()
-        c.n_seqs, c.max_pages = n, pages.shape[1]
+        i32, dev = self.torch.int32, self._index
+        n, most = pages.shape
+        assert pages.dtype is i32 and lens.dtype is i32 and row_start.dtype is i32
+        assert pages.get_device() == dev and lens.get_device() == dev and row_start.get_device() == dev
+        assert lens.shape == (n,) and row_start.shape == (n + 1,) and pages.is_contiguous() and lens.is_contiguous() and row_start.is_contiguous()
+        c = ArmtKvCache.from_buffer_copy(self._c)
+        c.pages, c.lens, c.row_start, c.n_seqs, c.max_pages = pages.data_ptr(), lens.data_ptr(), row_start.data_ptr(), n, most
         return c
+
+    def _out(self, out, n):
+        if out is None:
+            return self.torch.empty((n, self._q_width), dtype=self.act_dtype, device=self.device)
+        assert out.get_device() == self._index and out.dtype is self.act_dtype and out.shape == (n, self._q_width) and out.is_contiguous()
+        return out
 
     def append(self, qkv, pages, lens, row_start, positions=None, out=None):
         """qkv [n_rows, (H + 2 Hkv) dh] (rows may lie further apart): keys, rotated, and values into the cache; returns the rotated q
         [n_rows, H dh].  positions [n_rows] int32, or None: lens[s] + i."""
-        torch = self.torch
-        assert qkv.device == self.device and qkv.dtype == self.act_dtype and qkv.dim() == 2 and qkv.shape[1] == self._width and qkv.stride(1) == 1
-        n = qkv.shape[0]
+        torch, dev = self.torch, self._index
+        if torch._C._cuda_getDevice() != dev:
+            return _on_device(torch, dev, self.append, qkv, pages, lens, row_start, positions, out)
+        n, width = qkv.shape
+        ld, unit = qkv.stride()
+        assert qkv.get_device() == dev and qkv.dtype is self.act_dtype and width == self._width and unit == 1
         c = self._call(pages, lens, row_start)
+        at = None
         if positions is not None:
-            assert positions.device == self.device and positions.dtype == torch.int32 and positions.shape == (n,) and positions.is_contiguous()
-        with _on(torch, self.device):
-            if out is None:
-                out = torch.empty((n, self._q_width), dtype=self.act_dtype, device=self.device)
-            else:
-                assert out.device == self.device and out.dtype == self.act_dtype and out.shape == (n, self._q_width) and out.is_contiguous()
-            _check(self.lib, self.lib.armt_kv_append(self._cfg_ref, C.byref(c), qkv.data_ptr(), qkv.stride(0) if n > 1 else self._width, n,
-                                                     None if positions is None else positions.data_ptr(), out.data_ptr(),
-                                                     _raw_stream(torch, self.device)))
+            assert positions.get_device() == dev and positions.dtype is torch.int32 and positions.shape == (n,) and positions.is_contiguous()
+            at = positions.data_ptr()
+        out = self._out(out, n)
+        _check(self.lib, self.lib.armt_kv_append(self._cfg_ref, C.byref(c), qkv.data_ptr(), ld if n > 1 else width, n, at, out.data_ptr(),
+                                                 torch._C._cuda_getCurrentRawStream(dev)))
         return out
 
     def attend(self, q, pages, lens, row_start, max_rows, tree=None, out=None):
         """Attention of the rotated rows q [n_rows, H dh] over the cache, their own appended keys included -> [n_rows, H dh].
         max_rows: at least the rows of any sequence.  tree [n_rows] int64: bit j of a row's word: it sees key j of its sequence's rows
         (itself and its ancestors in a tree of drafts); None: rows see those up to themselves."""
-        torch = self.torch
-        assert q.device == self.device and q.dtype == self.act_dtype and q.dim() == 2 and q.shape[1] == self._q_width and q.is_contiguous()
-        n = q.shape[0]
+        torch, dev = self.torch, self._index
+        if torch._C._cuda_getDevice() != dev:
+            return _on_device(torch, dev, self.attend, q, pages, lens, row_start, max_rows, tree, out)
+        n, width = q.shape
+        assert q.get_device() == dev and q.dtype is self.act_dtype and width == self._q_width and q.is_contiguous()
         c = self._call(pages, lens, row_start)
+        words = None
         if tree is not None:
-            assert tree.device == self.device and tree.dtype == torch.int64 and tree.shape == (n,) and tree.is_contiguous()
+            assert tree.get_device() == dev and tree.dtype is torch.int64 and tree.shape == (n,) and tree.is_contiguous()
+            words = tree.data_ptr()
         need = self.lib.armt_kv_attention_workspace_bytes(self._cfg_ref, c.n_seqs, c.max_pages, self.page_len, n, max_rows)
         if need == 0:
             raise ArmtError(2, "configuration or sizes rejected by armt_kv_attention_workspace_bytes")
-        with _on(torch, self.device):
-            ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            if out is None:
-                out = torch.empty((n, self._q_width), dtype=self.act_dtype, device=self.device)
-            else:
-                assert out.device == self.device and out.dtype == self.act_dtype and out.shape == q.shape and out.is_contiguous()
-            _check(self.lib, self.lib.armt_kv_attention(self._cfg_ref, C.byref(c), q.data_ptr(), n, max_rows, None if tree is None else tree.data_ptr(),
-                                                        out.data_ptr(), ws.data_ptr(), need, _raw_stream(torch, self.device)))
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        out = self._out(out, n)
+        _check(self.lib, self.lib.armt_kv_attention(self._cfg_ref, C.byref(c), q.data_ptr(), n, max_rows, words, out.data_ptr(), ws.data_ptr(), need,
+                                                    torch._C._cuda_getCurrentRawStream(dev)))
         return out
 
 
@@ -580,21 +584,25 @@ def beam_select(logits, scores, n_out):
     """logits [n_seqs * n_beams, vocab] fp32 (rows may lie further apart), scores [n_seqs, n_beams] fp32 -> (scores, parents, tokens) of the n_out
     best continuations of every sequence, [n_seqs, n_out] fp32, int32, int32 (armt_beam_select)."""
     import torch
-    lib = load_library()
+    lib, dev = load_library(), logits.get_device()
+    assert dev >= 0
+    if torch._C._cuda_getDevice() != dev:
+        return _on_device(torch, dev, beam_select, logits, scores, n_out)
     n, beams = scores.shape
     rows, vocab = logits.shape
-    device = logits.device
-    assert logits.is_cuda and logits.dtype == torch.float32 and rows == n * beams and logits.stride(1) == 1
-    assert scores.device == device and scores.dtype == torch.float32 and scores.is_contiguous()
+    ld, unit = logits.stride()
+    assert logits.dtype is torch.float32 and rows == n * beams and (unit == 1 or vocab == 1)
+    assert scores.get_device() == dev and scores.dtype is torch.float32 and scores.is_contiguous()
     need = lib.armt_beam_select_workspace_bytes(n, beams, vocab, n_out)
     if need == 0:
         raise ArmtError(2, "sizes rejected by armt_beam_select_workspace_bytes")
-    with _on(torch, device):
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-        best = torch.empty((n, n_out), dtype=torch.float32, device=device)
-        parents, tokens = (torch.empty((n, n_out), dtype=torch.int32, device=device) for _ in range(2))
-        _check(lib, lib.armt_beam_select(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, scores.data_ptr(), n, beams, vocab, n_out,
-                                         best.data_ptr(), parents.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, _raw_stream(torch, device)))
+    device = logits.device
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    best = torch.empty((n, n_out), dtype=torch.float32, device=device)
+    parents = torch.empty((n, n_out), dtype=torch.int32, device=device)
+    tokens = torch.empty((n, n_out), dtype=torch.int32, device=device)
+    _check(lib, lib.armt_beam_select(logits.data_ptr(), ld if rows > 1 else vocab, scores.data_ptr(), n, beams, vocab, n_out, best.data_ptr(),
+                                     parents.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need, torch._C._cuda_getCurrentRawStream(dev)))
     return best, parents, tokens
 
 
@@ -603,31 +611,34 @@ def beam_reorder(parents, states, out=None):
     (n_seqs, n_beams), rows dense inside.  Returns the states of the beams that each beam continues: new tensors, or those in `out`, which may be
     the states themselves."""
     import torch
-    lib = load_library()
+    lib, dev = load_library(), parents.get_device()
+    assert dev >= 0
+    if torch._C._cuda_getDevice() != dev:
+        return _on_device(torch, dev, beam_reorder, parents, states, out)
     n, beams = parents.shape
-    rows, device = n * beams, parents.device
-    assert parents.is_cuda and parents.dtype == torch.int32 and parents.is_contiguous()
-    with _on(torch, device):
-        if out is None:
-            out = [torch.empty(t.shape, dtype=t.dtype, device=device) for t in states]
-        assert len(out) == len(states)
-        c = (ArmtBeamState * len(states))()
-        for s, t, o in zip(c, states, out):
-            assert t.device == device and o.device == device and t.dtype == o.dtype and t.shape == o.shape
-            size = t.element_size()
-            s.src, s.dst, s.row_bytes = t.data_ptr(), o.data_ptr(), t.numel() // rows * size
-            s.src_stride, s.dst_stride = _row_stride(t, n, beams) * size, _row_stride(o, n, beams) * size
-        _check(lib, lib.armt_beam_reorder(parents.data_ptr(), n, beams, c, len(states), _raw_stream(torch, device)))
+    rows = n * beams
+    assert parents.dtype is torch.int32 and parents.is_contiguous()
+    if out is None:
+        out = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in states]
+    assert len(out) == len(states)
+    c = (ArmtBeamState * len(states))()
+    for s, t, o in zip(c, states, out):
+        assert t.get_device() == dev and o.get_device() == dev and t.dtype is o.dtype and t.shape == o.shape
+        size = t.element_size()
+        s.src, s.dst, s.row_bytes = t.data_ptr(), o.data_ptr(), t.numel() // rows * size
+        s.src_stride, s.dst_stride = _row_stride(t, n, beams) * size, _row_stride(o, n, beams) * size
+    _check(lib, lib.armt_beam_reorder(parents.data_ptr(), n, beams, c, len(states), torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
 def _row_stride(t, n, beams):
     """Elements from one beam's row to the next of a state with n * beams rows."""
+    lead = t.shape[0]
+    assert lead == n * beams or (lead == n and t.shape[1] == beams)
     if t.is_contiguous():
-        assert t.shape[0] == n * beams or tuple(t.shape[:2]) == (n, beams)
         return t.numel() // (n * beams)
-    if t.shape[0] != n * beams:
-        assert tuple(t.shape[:2]) == (n, beams) and (n == 1 or beams == 1 or t.stride(0) == beams * t.stride(1))
+    if lead != n * beams:
+        assert n == 1 or beams == 1 or t.stride(0) == beams * t.stride(1)
         t = t[0] if n == 1 else t[:, 0] if beams == 1 else t.flatten(0, 1)
     assert t[0].is_contiguous()
     return t.stride(0)
