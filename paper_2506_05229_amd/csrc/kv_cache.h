@@ -785,6 +785,9 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   const int resident = p.shared ? (p.DH == 64 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
   int64_t spare = (target ? target : KA_CUS * resident) / ((int64_t)Hkv * p.blocks);
   if (spare > n_seqs * (steps - 1)) spare = n_seqs * (steps - 1);         // cuts that keys could be made at
+  // Short caches of one row tile are not cut: a second launch costs more than the walk through ten steps, sixteen where the workgroups are
+  // many (us, cut and joined / whole: 1 x 1040 keys 6.4 + 3.8 / 9.9, 1 x 2000 7.2 + 3.8 / 13.4, 8 x 2000 11.5 + 4.0 / 14.2, 32 x 2000 27.1 + 4.8 / 27.6)
+  if (!p.shared && p.QT == 1 && (steps <= 10 || (steps <= 16 && (int64_t)n_seqs * Hkv * p.blocks >= 64))) spare = 0;
   p.spare = (int)(spare < 0 ? 0 : spare);
   p.slots = n_seqs + p.spare;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
