@@ -264,20 +264,16 @@ struct KvTile {
 // A sequence's page table, read by scalar loads: the compiler's wait for a vector load would also wait for every copy in flight.
 typedef const __attribute__((address_space(4))) int32_t* kv_table_t;
 
-// Page bookkeeping of a wave's tile: base offsets (elements) of its 16-key halves, and which keys exist.
+// Where a tile's 16-key halves are: byte offsets from head kvh of page 0, and whether each of them lies on a page (bit h).
 template <typename T, int DH>
 struct KvHalves {
   static constexpr int N = KvTile<T, DH>::KEYS / 16;
   int64_t off[N];
-  unsigned have;      // bit h: half h lies on a page
+  int have;
 };
 
-// A value that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
-
-// The table's entries for a tile's halves, as they are: nothing waits for them before they are used, a tile later.
+// The table's entries for a tile's halves, as they are: nothing waits for them before they are used, a tile later.  Pages of 32 keys and more hold
+// both halves.
 template <typename T, int DH>
 struct KvEntries { int page[KvHalves<T, DH>::N], key0; };
 
@@ -285,21 +281,34 @@ template <typename T, int DH>
 __device__ __forceinline__ KvEntries<T, DH> kv_entries(const KvView& c, kv_table_t table, int key0) {
   KvEntries<T, DH> e;
   e.key0 = key0;
-#pragma unroll
-  for (int h = 0; h < KvHalves<T, DH>::N; ++h) e.page[h] = table[min((key0 + 16 * h) >> c.page_shift, c.max_pages - 1)];
+  e.page[0] = table[min(key0 >> c.page_shift, c.max_pages - 1)];
+  if constexpr (KvHalves<T, DH>::N > 1) {
+    e.page[1] = 0;
+    if (c.page_shift == 4) e.page[1] = table[min((key0 >> 4) + 1, c.max_pages - 1)];
+  }
   return e;
 }
 
+// (Halves behind the last key may lie on any page: their keys are not looked at.  A half without a page is read from page 0.)
 template <typename T, int DH>
-__device__ __forceinline__ KvHalves<T, DH> kv_halves(const KvView& c, const KvEntries<T, DH>& e, int total, int kvh, int dh) {
+__device__ __forceinline__ KvHalves<T, DH> kv_halves(const KvView& c, const KvEntries<T, DH>& e, int dh) {
   KvHalves<T, DH> r;
-  r.have = 0;
-#pragma unroll
-  for (int h = 0; h < KvHalves<T, DH>::N; ++h) {
-    const int key = e.key0 + 16 * h, page = __builtin_amdgcn_readfirstlane(e.page[h]);
-    const bool ok = key < total && page >= 0 && page < c.n_pages;
-    r.have |= ok ? 1u << h : 0u;
-    r.off[h] = uniform64((int64_t)(ok ? page : 0) * c.page_stride + (int64_t)((kvh << c.page_shift) + (key & ((1 << c.page_shift) - 1))) * dh);
+  const uint64_t stride = (uint64_t)c.page_stride * sizeof(T);
+  const unsigned row = (unsigned)dh * sizeof(T);
+  const unsigned p0 = __builtin_amdgcn_readfirstlane(e.page[0]);
+  const int ok0 = p0 < (unsigned)c.n_pages ? 1 : 0;
+  r.off[0] = (int64_t)((ok0 ? p0 : 0u) * stride + ((unsigned)e.key0 & ((1u << c.page_shift) - 1)) * row);
+  r.have = ok0;
+  if constexpr (KvHalves<T, DH>::N > 1) {
+    if (c.page_shift == 4) {
+      const unsigned p1 = __builtin_amdgcn_readfirstlane(e.page[1]);
+      const int ok1 = p1 < (unsigned)c.n_pages ? 1 : 0;
+      r.off[1] = (int64_t)((ok1 ? p1 : 0u) * stride);
+      r.have |= ok1 * 2;
+    } else {
+      r.off[1] = r.off[0] + 16 * row;
+      r.have *= 3;
+    }
   }
   return r;
 }
@@ -396,6 +405,8 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
   constexpr int PER = L::COPIES / KvHalves<T, DH>::N;       // copies of K, and of V, per 16-key half
   constexpr int NV = SHARED ? NCOPY : 2 * PER;              // a lane's offsets from the half's base; the swizzles repeat every 16 rows
   const int crow = lane / L::CHUNKS, cchunk = lane % L::CHUNKS;
+  const char* khead = (const char*)(kc + ((int64_t)kvh << c.page_shift) * dh);       // of this KV head in page 0
+  const char* vhead = (const char*)(vc + ((int64_t)kvh << c.page_shift) * dh);
   const unsigned char* ring = smem + (SHARED ? 0 : wave * (S * STAGE));
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) const void*)ring;
   unsigned voff[NV];
@@ -412,8 +423,8 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
     for (int x = 0; x < NCOPY; ++x) {
       const int y = SHARED ? wave * NCOPY + x : x, z = y % L::COPIES;
       const bool is_v = y >= L::COPIES;
-      const int64_t off = (KvHalves<T, DH>::N == 1 || z / PER == 0 ? hv.off[0] : hv.off[KvHalves<T, DH>::N - 1]) * (int)sizeof(T);
-      lds_copy16((const char*)(is_v ? vc : kc) + off, voff[SHARED ? x : (y / L::COPIES) * PER + z % PER], lds0 + stage * STAGE + y * 1024);
+      const int64_t off = KvHalves<T, DH>::N == 1 || z / PER == 0 ? hv.off[0] : hv.off[KvHalves<T, DH>::N - 1];
+      lds_copy16((is_v ? vhead : khead) + off, voff[SHARED ? x : (y / L::COPIES) * PER + z % PER], lds0 + stage * STAGE + y * 1024);
     }
   };
 
@@ -429,21 +440,22 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
 
   const int key_first = sq.first + (SHARED ? 0 : wave * KEYS), stride = TILE_WAVES * KEYS;
   const int n = last > key_first ? (last - key_first + stride - 1) / stride : 0;
-  unsigned have[S];
+  int have[S];
 #pragma unroll
   for (int x = 0; x < S - 1; ++x)
     if (x < n) {
-      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, kv_entries<T, DH>(c, table, key_first + x * stride), sq.total, kvh, dh);
+      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, kv_entries<T, DH>(c, table, key_first + x * stride), dh);
       have[x] = hv.have;
       issue(hv, x);
     }
 
   bool any_odd = false;       // values that are not finite were left out
-  auto tile = [&](int it, int stage, unsigned pages_ok) __attribute__((always_inline)) {
+  const int whole_until = min(sq.len, last);
+  auto tile = [&](int it, int stage, int pages_ok) __attribute__((always_inline)) {
     unsigned char* Kt = (unsigned char*)ring + stage * STAGE;
     unsigned char* Vt = Kt + L::BYTES;
     const int key0 = key_first + it * stride;
-    const bool edge = key0 + KEYS > min(sq.len, last) || pages_ok != (1u << KvHalves<T, DH>::N) - 1;       // (uniform) some key is not everybody's
+    const bool edge = key0 + KEYS > whole_until || pages_ok != (1 << KvHalves<T, DH>::N) - 1;       // (uniform) some key is not everybody's
     const unsigned exist = keys_below(sq.total, key0) & ((pages_ok & 1 ? 0xffffu : 0u) | (pages_ok & 2 ? 0xffff0000u : 0u));
     if (edge) {
       // Values of keys that do not exist become zero, since 0 x NaN is not.  So do, of the call's own keys, which some rows see and others do
@@ -569,13 +581,21 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
       }
       lsum[t] += hs;
       if constexpr (BF) {
-        bf16x8 pf;
+        // P in bf16, as the operand of the matrix product: half a step of 2^-8 each.  For one row tile, where the keys' bytes are what takes time, what the
+        // rounding leaves follows as a second operand (48 sequences 106 us with and without, the short walk over 1040 keys 10.1 -> 10.6).
+        bf16x8 pf, rest;
 #pragma unroll
         for (int a = 0; a < 2; ++a)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) pf[a * 4 + r] = (bf16)pr[a][r];      // P in bf16: 2^-9 relative, as the operand of the matrix product
+          for (int r = 0; r < 4; ++r) {
+            pf[a * 4 + r] = (bf16)pr[a][r];
+            if constexpr (QT == 1 && !SHARED) rest[a * 4 + r] = (bf16)(pr[a][r] - (float)pf[a * 4 + r]);
+          }
 #pragma unroll
-        for (int d = 0; d < NT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
+        for (int d = 0; d < NT; ++d) {
+          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
+          if constexpr (QT == 1 && !SHARED) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], rest, o[t][d], 0, 0, 0);
+        }
       } else {
 #pragma unroll
         for (int d = 0; d < NT; ++d)
@@ -605,7 +625,7 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
     auto next = [&]() __attribute__((always_inline)) {
       int into = stage + S - 1;
       into = into >= S ? into - S : into;
-      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, nx, sq.total, kvh, dh);
+      const KvHalves<T, DH> hv = kv_halves<T, DH>(c, nx, dh);
       have[S - 1] = hv.have;
       issue(hv, into);
       nx = kv_entries<T, DH>(c, table, key_first + (it + S) * stride);
@@ -784,6 +804,9 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   // workgroups wanted: what the chip holds at once
   const int resident = p.shared ? (p.DH == 64 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
   int64_t spare = (target ? target : KA_CUS * resident) / ((int64_t)Hkv * p.blocks);
+  // ... and twice that where sequences of uneven length and 128 dimensions share it (a workgroup's walk is longest there): 16 trees of up to 48 drafts of 24 / 8
+  // heads 90 -> 77 us, 32 of 16 of 32 / 8 70.7 -> 64.2; at 64 dimensions no better
+  if (p.shared && p.DH == 128 && n_seqs * 4 > spare) spare *= 2;
   if (spare > n_seqs * (steps - 1)) spare = n_seqs * (steps - 1);         // cuts that keys could be made at
   // Short caches of one row tile are not cut: a second launch costs more than the walk through ten steps, sixteen where the workgroups are
   // many (us, cut and joined / whole: 1 x 1040 keys 6.4 + 3.8 / 9.9, 1 x 2000 7.2 + 3.8 / 13.4, 8 x 2000 11.5 + 4.0 / 14.2, 32 x 2000 27.1 + 4.8 / 27.6)
