@@ -152,6 +152,7 @@ inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const K
 constexpr int KA_WAVES = 4;
 constexpr int KA_STEP = 128;              // keys are cut into slots at multiples of this
 constexpr int KA_CUS = 256;               // compute units
+constexpr int KA_FEW = 512;               // keys of a sequence up to which the probabilities are not rounded
 constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
 
 struct KvSeq { int s, len, row0, rows, all, total, first, last, count, slot0; };   // keys of a slot: [first, last)
@@ -451,6 +452,7 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
 
   bool any_odd = false;       // values that are not finite were left out
   const int whole_until = min(sq.len, last);
+  const bool few_keys = sq.total <= KA_FEW;
   auto tile = [&](int it, int stage, int pages_ok) __attribute__((always_inline)) {
     unsigned char* Kt = (unsigned char*)ring + stage * STAGE;
     unsigned char* Vt = Kt + L::BYTES;
@@ -581,20 +583,22 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
       }
       lsum[t] += hs;
       if constexpr (BF) {
-        // P in bf16, as the operand of the matrix product: half a step of 2^-8 each.  For one row tile, where the keys' bytes are what takes time, what the
-        // rounding leaves follows as a second operand (48 sequences 106 us with and without, the short walk over 1040 keys 10.1 -> 10.6).
-        bf16x8 pf, rest;
+        // P in bf16, as the operand of the matrix product: half a step of 2^-8 each.  Where the keys' bytes are what takes time (one row tile: 48 sequences
+        // 106 us with and without) and where keys are few, so that single roundings show, what they leave follows as a second operand.
+        bf16x8 pf;
 #pragma unroll
         for (int a = 0; a < 2; ++a)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            pf[a * 4 + r] = (bf16)pr[a][r];
-            if constexpr (QT == 1 && !SHARED) rest[a * 4 + r] = (bf16)(pr[a][r] - (float)pf[a * 4 + r]);
-          }
+          for (int r = 0; r < 4; ++r) pf[a * 4 + r] = (bf16)pr[a][r];
 #pragma unroll
-        for (int d = 0; d < NT; ++d) {
-          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
-          if constexpr (QT == 1 && !SHARED) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], rest, o[t][d], 0, 0, 0);
+        for (int d = 0; d < NT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
+        if ((QT == 1 && !SHARED) || few_keys) {
+#pragma unroll
+          for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) pf[a * 4 + r] = (bf16)(pr[a][r] - (float)pf[a * 4 + r]);
+#pragma unroll
+          for (int d = 0; d < NT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
         }
       } else {
 #pragma unroll
@@ -804,9 +808,9 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   // workgroups wanted: what the chip holds at once
   const int resident = p.shared ? (p.DH == 64 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
   int64_t spare = (target ? target : KA_CUS * resident) / ((int64_t)Hkv * p.blocks);
-  // ... and twice that where sequences of uneven length and 128 dimensions share it (a workgroup's walk is longest there): 16 trees of up to 48 drafts of 24 / 8
-  // heads 90 -> 77 us, 32 of 16 of 32 / 8 70.7 -> 64.2; at 64 dimensions no better
-  if (p.shared && p.DH == 128 && n_seqs * 4 > spare) spare *= 2;
+  // ... and twice that where many sequences of 128 dimensions share it (a workgroup's walk is longest there, and uneven): 16 trees of up to 48 drafts of 24 / 8
+  // heads 90 -> 77 us, 32 of 16 of 32 / 8 70.7 -> 64.2; two chains of 300 rows 101 -> 110, at 64 dimensions no better
+  if (p.shared && p.DH == 128 && n_seqs >= 8 && n_seqs * 4 > spare) spare *= 2;
   if (spare > n_seqs * (steps - 1)) spare = n_seqs * (steps - 1);         // cuts that keys could be made at
   // Short caches of one row tile are not cut: a second launch costs more than the walk through ten steps, sixteen where the workgroups are
   // many (us, cut and joined / whole: 1 x 1040 keys 6.4 + 3.8 / 9.9, 1 x 2000 7.2 + 3.8 / 13.4, 8 x 2000 11.5 + 4.0 / 14.2, 32 x 2000 27.1 + 4.8 / 27.6)

@@ -90,17 +90,20 @@ class Problem:
         page = page.clamp(0, self.k.shape[0] - 1)
         return self.k[page, :, t % self.page].double(), self.v[page, :, t % self.page].double(), have
 
-    def attend(self, q, tree=None, max_rows=None):
-        """Output, and a bound of the kernel's rounding, per element (rows that nobody owns: NaN).
+    def attend(self, q, tree=None, max_rows=None, called=None):
+        """Output, and a bound of the kernel's rounding, per element (rows that nobody owns: NaN).  called: the max_rows of the call.
 
-        The bound counts half steps.  Output: one of its type.  Second product: every probability rounded once (bf16) or exact in fp32,
-        so at most a half step of sum p |v|.  In fp32, with u = 2^-24: a score of dh products is off by (dh + 4) u sum |q k| / sqrt(dh), the exponential by
+        The bound counts half steps.  Output: one of its type.  Second product in bf16: every probability rounded once, so at most a half step of
+        sum p |v|, or twice (the rest of the first rounding) for few keys or rows: a half step of a half step.  In fp32, with u = 2^-24: a score of dh products is off by (dh + 4) u sum |q k| / sqrt(dh), the exponential by
         3 u, sums over n keys by (n + 8) u; each moves the result by at most twice that share of sum p |v|."""
         H, Hkv, dh, u = self.H, self.Hkv, self.dh, 2.0 ** -24
+        called = called or max_rows or max(self.rows)
         out = torch.full((self.n_rows, H, dh), float("nan"), dtype=torch.float64)
         tol = torch.zeros_like(out)
         for s in range(len(self.lens)):
             k, v, have = self.keys_of(s)
+            half = HALF_STEP[self.dt]
+            half_p = 0 if self.dt == torch.float32 else half * half if called * H // Hkv <= 16 or len(have) <= 512 else half
             for i in range(self.rows[s] if max_rows is None else min(self.rows[s], max_rows)):
                 r = int(self.row_start[s]) + i
                 see = have.clone()
@@ -118,8 +121,7 @@ class Problem:
                     out[r, h] = p @ vv[:, h * Hkv // H]
                     spread = p @ vv[:, h * Hkv // H].abs()
                     off = (kk[:, h * Hkv // H].abs() @ qq.abs()).max() / math.sqrt(dh) * (dh + 4) * u + (len(kk) + 11) * u
-                    half = HALF_STEP[self.dt]
-                    tol[r, h] = half * out[r, h].abs() + spread * (2 * off + (half if self.dt == torch.bfloat16 else 0)) * 1.02
+                    tol[r, h] = half * out[r, h].abs() + spread * (2 * off + half_p) * 1.02
         return out.view(self.n_rows, -1), tol.view(self.n_rows, -1)
 
 

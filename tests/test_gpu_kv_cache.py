@@ -119,11 +119,11 @@ def test_attention(heads, dtype, page, lens, rows, tree):
     pr.own_keys()
     q = pr.queries()
     words = pr.trees() if tree else None
-    want, tol = pr.attend(q, words)
     cache = pr.on_gpu()
     out = torch.full_like(q, 55.0).cuda()
     n = int(pr.row_start[-1])
     for max_rows in (max(rows), max(rows) + 3 if not tree else 64):
+        want, tol = pr.attend(q, words, called=max_rows)
         out.fill_(55.0)
         cache.attend(q.cuda(), *pr.args, max_rows, tree=None if words is None else words.cuda(), out=out)
         torch.cuda.synchronize()
