@@ -351,12 +351,13 @@ typedef struct {
 /* Rows of the fused projection into the cache, rotated on the way: q and k by their position as in armt_segment_attention, q_out [n_rows,
  * H * dh] = R(p) q, key lens[s] + i = R(p) k, its value v.  qkv: rows [q heads | k heads | v heads], ld_qkv elements apart.
  * positions [n_rows], or NULL for lens[s] + i (drafts of a tree that share a depth share a position).  A row whose key has no page gets its
- * q_out all the same.  No workspace. */
+ * q_out all the same.  q_out must not overlap qkv (ARMT_ERR_SHAPE).  No workspace. */
 armt_status armt_kv_append(const armt_config *cfg, const armt_kv_cache *cache, const void *qkv, int64_t ld_qkv, int32_t n_rows,
                            const int32_t *positions, void *q_out, void *hip_stream);
 
 /* Attention of the rows over the cache, their own keys (appended before) included: out[r][h] = softmax over the keys that row r sees
- * (q[r][h] . k / sqrt(dh)) times v, grouped-query heads; q [n_rows, H * dh] rotated (q_out of armt_kv_append), out the same shape.
+ * (q[r][h] . k / sqrt(dh)) times v, grouped-query heads; q [n_rows, H * dh] rotated (q_out of armt_kv_append), out the same shape and
+ * elsewhere (ARMT_ERR_SHAPE).
  * Every row sees the lens[s] keys in front.  Of the call's own keys, row i sees key j iff bit j of tree[r] is set (a tree of
  * drafted tokens: itself and its ancestors; at most 64 rows per sequence), or without a tree (NULL) iff j <= i (one token, or a chain).
  * What a row does not see has no influence on it, not even a NaN; a row that sees no key is zero.  max_rows: at least the
@@ -374,7 +375,8 @@ armt_status armt_kv_attention(const armt_config *cfg, const armt_kv_cache *cache
  * logits [n_seqs * n_beams] rows ld_logits apart (fp32, as armt_lm_head writes them), scores [n_seqs, n_beams]; out_scores,
  * out_parents (beam), out_tokens [n_seqs, n_out].  A logit of -inf bans a token, a score of -inf a beam (the first step has one live
  * beam): such continuations come last, with score -inf.  NaN logits count as -inf, +inf as the largest finite number; a score
- * that is not finite counts as -inf, and so do all of a beam without a logit above -inf.
+ * that is not finite counts as -inf, and so do all of a beam without a logit above -inf.  out_scores may be scores where n_out == n_beams; no other
+ * output may overlap them (ARMT_ERR_SHAPE).
  * Supported: n_out <= 64, n_beams <= 64, n_beams * vocab <= 2^31 - 2^16, n_seqs * n_beams < 2^24. */
 size_t armt_beam_select_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out);
 armt_status armt_beam_select(const float *logits, int64_t ld_logits, const float *scores, int32_t n_seqs, int32_t n_beams, int32_t vocab,

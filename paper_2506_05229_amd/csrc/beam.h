@@ -20,6 +20,7 @@ constexpr int BS_BEAMS = 64;           // beams of a sequence
 constexpr int BS_WAVES = 4;
 constexpr int BS_CAP = 256;            // survivors a wave may have; with more (ties, mostly) it sorts by insertion
 constexpr int BS_PICK = 8;             // waves of the second launch
+constexpr int kMaxBlocks = 0xffffff;   // of 256 threads: a launch has fewer than 2^32
 
 struct BeamPart { double sum; float top; int pad; };      // of one workgroup's part of a row: sum of exp(x - top)
 
@@ -213,9 +214,9 @@ struct ScoreList {
   }
 };
 
-// grid: sequences, block: 512.
-__global__ __launch_bounds__(BS_PICK * 64) void beam_pick_kernel(const u64* __restrict__ list, const BeamPart* __restrict__ info, const float* __restrict__ scores,
-                                                                  int beams, int vocab, int n_out, int parts, float* __restrict__ out_scores,
+// out_scores may be scores: a workgroup has read its sequence's before it writes them.  grid: sequences, block: 512.
+__global__ __launch_bounds__(BS_PICK * 64) void beam_pick_kernel(const u64* __restrict__ list, const BeamPart* __restrict__ info, const float* scores,
+                                                                  int beams, int vocab, int n_out, int parts, float* out_scores,
                                                                   int32_t* __restrict__ out_parents, int32_t* __restrict__ out_tokens) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int CAP = BS_CAP + 4;
@@ -491,7 +492,7 @@ inline int64_t beam_reorder_blocks(BeamStates& st, int n_seqs, int unit) {
   int64_t grid = 0;
   for (int i = 0; i < st.n; ++i) {
     const int64_t cols = (st.s[i].row_bytes + 256 * unit - 1) / (256 * unit);
-    if (cols > 0x7fffffff / n_seqs || grid + cols * n_seqs > 0x7fffffff) return -1;
+    if (cols > kMaxBlocks / n_seqs || grid + cols * n_seqs > kMaxBlocks) return -1;
     st.s[i].first_block = (int)grid;
     st.s[i].cols = (int)cols;
     grid += cols * n_seqs;

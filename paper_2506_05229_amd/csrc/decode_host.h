@@ -27,7 +27,11 @@ armt_status check_cache(const armt_config* cfg, const armt_kv_cache* cache, int3
 bool attention_plan(const Dims& D, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t n_rows, int32_t max_rows, KvPlan* p) {
   if ((int64_t)max_rows * (D.H / D.Hkv) > 1 << 30) return false;
   *p = kv_plan(D.bf16, n_seqs, n_rows, max_rows, (int64_t)max_pages * page_len, D.H, D.Hkv, D.dh);
-  return kv_grid(*p, D.Hkv) <= 0x7fffffff && (int64_t)n_rows * D.H <= 0x7fffffff;
+  return kv_grid(*p, D.Hkv) <= kMaxBlocks && ((int64_t)n_rows * D.H + 3) / 4 <= kMaxBlocks;
+}
+
+bool ranges_meet(const void* a, int64_t la, const void* b, int64_t lb) {
+  return (uintptr_t)a < (uintptr_t)b + lb && (uintptr_t)b < (uintptr_t)a + la;
 }
 
 // Whether two sets of n rows may share memory (rows of equal stride may lie between each other).
@@ -51,6 +55,9 @@ armt_status armt_kv_append(const armt_config* cfg, const armt_kv_cache* cache, c
   if (!qkv || !q_out) return ARMT_ERR_NULL;
   if (ld_qkv < D.Nqkv) return ARMT_ERR_SHAPE;
   if (ld_qkv * (int64_t)D.esz % 16 || (uintptr_t)qkv % 16 || (uintptr_t)q_out % 16) return ARMT_ERR_UNSUPPORTED;
+  if (((int64_t)n_rows + KV_ROWS - 1) / KV_ROWS > kMaxBlocks) return ARMT_ERR_UNSUPPORTED;
+  const int64_t esz = D.esz;
+  if (ranges_meet(q_out, (int64_t)n_rows * D.H * D.dh * esz, qkv, ((int64_t)(n_rows - 1) * ld_qkv + D.Nqkv) * esz)) return ARMT_ERR_SHAPE;
   HIP_TRY(launch_kv_append(D.bf16, qkv, ld_qkv, v, positions, q_out, cache->k, cache->v, D.H, D.Hkv, D.dh, D.rope_theta, (hipStream_t)hip_stream));
   return ARMT_OK;
 }
@@ -73,6 +80,8 @@ armt_status armt_kv_attention(const armt_config* cfg, const armt_kv_cache* cache
   if (!q || !out) return ARMT_ERR_NULL;
   if (max_rows < 1 || (tree && max_rows > 64)) return ARMT_ERR_SHAPE;
   if ((uintptr_t)q % 16 || (uintptr_t)out % 16) return ARMT_ERR_UNSUPPORTED;
+  const int64_t bytes = (int64_t)n_rows * D.H * D.dh * (int64_t)D.esz;
+  if (ranges_meet(q, bytes, out, bytes)) return ARMT_ERR_SHAPE;
   if (!attention_plan(D, cache->n_seqs, cache->max_pages, cache->page_len, n_rows, max_rows, &p)) return ARMT_ERR_UNSUPPORTED;
   if (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < std::max(p.total, kAlign)) return ARMT_ERR_WORKSPACE;
   HIP_TRY(launch_kv_attention(D.bf16, p, q, cache->k, cache->v, (const unsigned long long*)tree, v, out, (char*)workspace, D.H, D.Hkv, D.dh, max_rows,
@@ -84,6 +93,7 @@ size_t armt_beam_select_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t
   if (n_seqs < 1 || n_beams < 1 || vocab < 1 || n_out < 1 || n_out > BS_MAX || n_beams > BS_BEAMS || (int64_t)n_beams * vocab < n_out ||
       (int64_t)n_beams * vocab > 0x7fff0000 || (int64_t)n_seqs * n_beams > 0xffffff)
     return 0;
+  if ((int64_t)n_seqs * n_beams * beam_parts((int64_t)n_seqs * n_beams, vocab) > kMaxBlocks || n_seqs > kMaxBlocks / 2) return 0;
   return beam_workspace((int64_t)n_seqs * n_beams, vocab, n_out);
 }
 
@@ -94,6 +104,9 @@ armt_status armt_beam_select(const float* logits, int64_t ld_logits, const float
   const size_t need = armt_beam_select_workspace_bytes(n_seqs, n_beams, vocab, n_out);
   if (!need) return ARMT_ERR_UNSUPPORTED;
   if (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < need) return ARMT_ERR_WORKSPACE;
+  const int64_t in = (int64_t)n_seqs * n_beams * 4, out = (int64_t)n_seqs * n_out * 4;
+  if (ranges_meet(out_scores, out, scores, in) && !((const float*)out_scores == scores && n_out == n_beams)) return ARMT_ERR_SHAPE;
+  if (ranges_meet(out_parents, out, scores, in) || ranges_meet(out_tokens, out, scores, in)) return ARMT_ERR_SHAPE;
   HIP_TRY(launch_beam_select(logits, ld_logits, scores, n_seqs, n_beams, vocab, n_out, out_scores, out_parents, out_tokens, (char*)workspace,
                              (hipStream_t)hip_stream));
   return ARMT_OK;

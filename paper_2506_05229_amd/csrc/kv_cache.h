@@ -48,6 +48,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qk
   __shared__ float cs[KV_ROWS][128];     // cos dh/2 | sin dh/2
   __shared__ int64_t at[KV_ROWS];        // element of the key in head 0 of its page; -1: no page; -2: nobody's row
   __shared__ int64_t slot[KV_ROWS];
+  __shared__ int near;
   const int half = dh >> 1, hv = half / VEC, rot_items = (H + Hkv) * hv, dv = dh / VEC, row_items = rot_items + Hkv * dv;
   const int tid = threadIdx.x, P = 1 << c.page_shift;
   const int64_t row0 = (int64_t)blockIdx.x * per;
@@ -73,9 +74,21 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const T* __restrict__ qk
   static_assert(KV_ROWS * 64 <= 256, "an angle per thread");
   const int ar = tid / half, aj = tid - ar * half, pos = positions && ar < rows ? positions[row0 + ar] : 0;
   if (tid < KV_ROWS) { at[tid] = -2; slot[tid] = 0; }
+  if (tid == 0) near = 0;
   __syncthreads();
-  for (int s = tid; s < c.n_seqs; s += 256) {
+  // whose rows these are: the sequences from the last one that starts at or before row0 to the first that starts behind them
+  int from = 0;
+  for (int n = c.n_seqs; n > 256;) {     // of many sequences, 256 at equal distances at a time
+    const int step = (n + 255) / 256, s = from + tid * step;
+    if (tid * step < n && c.row_start[s] <= row0) atomicMax(&near, s);
+    __syncthreads();
+    n = min(step, n - (max(near, from) - from));
+    from = max(near, from);
+    __syncthreads();
+  }
+  for (int s = from + tid; s < c.n_seqs; s += 256) {
     const int64_t lo = c.row_start[s], hi = c.row_start[s + 1], len = c.lens[s];
+    if (lo >= row0 + rows) break;
     for (int64_t r = max(lo, row0); r < min(hi, row0 + rows); ++r) {
       const int64_t k = len + (r - lo), j = k >> c.page_shift;
       const int page = k >= 0 && j < c.max_pages ? c.pages[(int64_t)s * c.max_pages + j] : -1;
@@ -152,6 +165,7 @@ inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const K
 constexpr int KA_WAVES = 4;
 constexpr int KA_STEP = 128;              // keys are cut into slots at multiples of this
 constexpr int KA_CUS = 256;               // compute units
+constexpr int KA_PLANNED = 1024;          // sequences up to which long ones are cut: every workgroup looks at all lengths
 constexpr int KA_FEW = 512;               // keys of a sequence up to which the probabilities are not rounded
 constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
 
@@ -815,6 +829,9 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   // Short caches of one row tile are not cut: a second launch costs more than the walk through ten steps, sixteen where the workgroups are
   // many (us, cut and joined / whole: 1 x 1040 keys 6.4 + 3.8 / 9.9, 1 x 2000 7.2 + 3.8 / 13.4, 8 x 2000 11.5 + 4.0 / 14.2, 32 x 2000 27.1 + 4.8 / 27.6)
   if (!p.shared && p.QT == 1 && (steps <= 10 || (steps <= 16 && (int64_t)n_seqs * Hkv * p.blocks >= 64))) spare = 0;
+  // Nor are those of very many sequences: a workgroup would spend its time on the lengths (us, n sequences of 300 keys and one of 60000, cut / whole:
+  // 520 125 / 299, 1024 270 / 322, 4096 2549 / 501; 1024 with eight of 20000 304 / 258)
+  if (n_seqs > KA_PLANNED) spare = 0;
   p.spare = (int)(spare < 0 ? 0 : spare);
   p.slots = n_seqs + p.spare;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };

@@ -8,7 +8,8 @@ import armt_synth as S
 
 HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}      # half a step relative to the value
 HEADS = {"tiny": (4, 2, 32), "narrow": (6, 3, 20), "wide": (4, 1, 100), "160m": (12, 12, 64), "1b": (32, 8, 64), "3b": (24, 8, 128), "8b": (32, 8, 128),
-         "one": (8, 1, 64)}
+         "one": (8, 1, 64),
+         "mini": (3, 1, 4), "eight": (2, 2, 8), "twelve": (4, 2, 12)}
 
 
 def cache_shape(heads, dtype, theta=500000.0):

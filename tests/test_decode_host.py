@@ -61,12 +61,12 @@ def test_fp32_head_sizes(lib):
 
 def test_append_refusals(lib):
     c, k = cfg(), cache()
-    call = lambda qkv=FAKE, ld=48 * 64, n=5, out=FAKE: lib.armt_kv_append(C.byref(c), C.byref(k), qkv, ld, n, None, out, None)  # noqa: E731
+    call = lambda qkv=FAKE, ld=48 * 64, n=5, out=FAKE + (1 << 20): lib.armt_kv_append(C.byref(c), C.byref(k), qkv, ld, n, None, out, None)  # noqa: E731
     assert lib.armt_kv_append(None, C.byref(k), FAKE, 48 * 64, 5, None, FAKE, None) == NULL
     assert lib.armt_kv_append(C.byref(c), None, FAKE, 48 * 64, 5, None, FAKE, None) == NULL
     assert call(qkv=None) == NULL and call(out=None) == NULL
     assert call(n=0) == SHAPE and call(ld=48 * 64 - 8) == SHAPE
-    assert call(ld=48 * 64 + 4) == UNSUPPORTED and call(qkv=FAKE + 4) == UNSUPPORTED and call(out=FAKE + 8) == UNSUPPORTED
+    assert call(ld=48 * 64 + 4) == UNSUPPORTED and call(qkv=FAKE + 4) == UNSUPPORTED and call(out=FAKE + (1 << 20) + 8) == UNSUPPORTED and call(out=FAKE + 4096) == SHAPE
 
 
 def test_attention_refusals(lib):
@@ -74,12 +74,12 @@ def test_attention_refusals(lib):
     need = lib.armt_kv_attention_workspace_bytes(C.byref(c), 2, 4, 64, 5, 3)
     assert need >= 256
 
-    def call(q=FAKE, n=5, rows=3, tree=None, out=FAKE, ws=FAKE, size=need):
+    def call(q=FAKE, n=5, rows=3, tree=None, out=FAKE + (1 << 20), ws=FAKE, size=need):
         return lib.armt_kv_attention(C.byref(c), C.byref(k), q, n, rows, tree, out, ws, size, None)
 
     assert call(q=None) == NULL and call(out=None) == NULL
     assert call(n=0) == SHAPE and call(rows=0) == SHAPE and call(rows=65, tree=FAKE, size=1 << 40) == SHAPE
-    assert call(q=FAKE + 8) == UNSUPPORTED and call(out=FAKE + 4) == UNSUPPORTED
+    assert call(q=FAKE + 8) == UNSUPPORTED and call(out=FAKE + (1 << 20) + 4) == UNSUPPORTED and call(out=FAKE + 64) == SHAPE
     assert call(ws=None) == WORKSPACE and call(ws=FAKE + 128) == WORKSPACE and call(size=need - 1) == WORKSPACE
     assert call(rows=2 ** 31 - 1, size=1 << 62) == UNSUPPORTED
 
@@ -98,15 +98,16 @@ def test_beam_select_refusals(lib):
     assert all(lib.armt_beam_select_workspace_bytes(*a) == 0 for a in ((0, 3, 9, 1), (2, 0, 9, 1), (2, 3, 0, 1), (2, 3, 9, 0), (2, 3, 9, 28), (2, 3, 999, 65),
                                                                       (1, 3, 2 ** 31 - 1, 6), (2 ** 24, 1, 9, 1)))
 
-    def call(x=FAKE, ld=1000, s=FAKE, n=2, beams=3, vocab=1000, n_out=6, o=(FAKE, FAKE, FAKE), ws=FAKE, size=need):
+    def call(x=FAKE, ld=1000, s=FAKE, n=2, beams=3, vocab=1000, n_out=6, o=(2 * FAKE, 3 * FAKE, 4 * FAKE), ws=FAKE, size=need):
         return lib.armt_beam_select(x, ld, s, n, beams, vocab, n_out, *o, ws, size, None)
 
     assert call(x=None) == NULL and call(s=None) == NULL
-    assert all(call(o=tuple(None if i == j else FAKE for i in range(3))) == NULL for j in range(3))
+    assert all(call(o=tuple(None if i == j else (2 + i) * FAKE for i in range(3))) == NULL for j in range(3))
     assert call(n=0) == SHAPE and call(beams=0) == SHAPE and call(vocab=0) == SHAPE and call(n_out=0) == SHAPE and call(ld=999) == SHAPE
     assert call(vocab=1, n_out=4) == SHAPE
     assert call(n_out=65) == UNSUPPORTED and call(beams=2 ** 22) == UNSUPPORTED
     assert call(ws=None) == WORKSPACE and call(ws=FAKE + 64) == WORKSPACE and call(size=need - 1) == WORKSPACE
+    assert all(call(o=tuple(FAKE if i == j else (2 + i) * FAKE for i in range(3))) == SHAPE for j in range(3))
 
 
 def test_beam_reorder_refusals(lib):

@@ -76,6 +76,25 @@ def test_equal_beams_tie_to_the_lowest():
     assert got[1][0].tolist() == [0, 1, 2, 3] * 3
 
 
+def test_scores_in_place():
+    import ctypes as C
+
+    import paper_2506_05229_amd as P
+    lib = P.load_library()
+    gen = torch.Generator().manual_seed(6)
+    x, scores = torch.randn(10, 700, generator=gen).cuda(), (-torch.rand(2, 5, generator=gen)).cuda()
+    want = P.beam_select(x, scores, 5)
+    parents, tokens = torch.empty(2, 5, dtype=torch.int32, device="cuda"), torch.empty(2, 5, dtype=torch.int32, device="cuda")
+    need = lib.armt_beam_select_workspace_bytes(2, 5, 700, 5)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    call = lambda n_out, out: lib.armt_beam_select(x.data_ptr(), 700, scores.data_ptr(), 2, 5, 700, n_out, out, parents.data_ptr(),  # noqa: E731
+                                                   tokens.data_ptr(), ws.data_ptr(), need, C.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert call(4, scores.data_ptr()) == 2 and call(5, scores.data_ptr() + 4) == 2
+    assert call(5, scores.data_ptr()) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(scores, want[0]) and torch.equal(parents, want[1]) and torch.equal(tokens, want[2])
+
+
 def test_select_and_reorder_replay_from_a_graph():
     import paper_2506_05229_amd as P
     gen = torch.Generator().manual_seed(4)

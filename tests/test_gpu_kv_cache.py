@@ -23,6 +23,11 @@ APPEND = [
     ("narrow", "f32", 16, [3, 15], [5, 2]),
     ("wide", "f32", 32, [1, 31], [3, 40]),
     ("8b", "f32", 64, [63], [2]),
+    ("mini", "f32", 16, [5, 0], [3, 20]),
+    ("eight", "f32", 16, [5, 15], [3, 2]),
+    ("twelve", "f32", 32, [31], [4]),
+    ("eight", "f32", 16, [s % 5 for s in range(700)], [s % 3 for s in range(700)]),        # more sequences than threads, empty ones among them
+    ("one", "bf16", 16, [3] * 300, [0] * 149 + [5] + [0] * 149 + [2]),
 ]
 
 
@@ -110,6 +115,10 @@ ATTEND = [
     ("wide", "f32", 16, [37, 100], [2, 11], False),
     ("1b", "f32", 64, [200], [5], True),
     ("8b", "f32", 32, [70, 3], [1, 30], False),
+    ("mini", "f32", 16, [50, 3], [2, 9], True),
+    ("eight", "f32", 16, [130, 0], [20, 1], False),
+    ("twelve", "f32", 32, [31, 64], [4, 1], True),
+    ("eight", "f32", 16, [s % 90 for s in range(600)], [s % 3 for s in range(600)], False),
 ]
 
 
@@ -304,3 +313,14 @@ def test_chain_of_one_token_calls_equals_one_call():
         got = cache.attend(cache.append(qkv[i:i + 1], pr.args[0], lens, one), pr.args[0], lens, one, 1)
         # both are within half a step of the output and of each probability
         assert_close(got[0], whole[i].double().cpu(), 2 * 2.0 ** -8 * (whole[i].double().cpu().abs() + 1.0), i)
+
+
+def test_outputs_over_inputs_are_refused():
+    import paper_2506_05229_amd as P
+    pr = Problem("tiny", "f32", 16, [20], [2])
+    cache, q = pr.on_gpu(), pr.queries().cuda()
+    with pytest.raises(P.ArmtError):
+        cache.attend(q, *pr.args, 2, out=q)
+    qkv = torch.randn(2, (pr.H + 2 * pr.Hkv) * pr.dh, generator=pr.gen).cuda()
+    with pytest.raises(P.ArmtError):
+        cache.append(qkv, *pr.args, out=qkv.view(-1)[:2 * pr.H * pr.dh].view(2, -1))
