@@ -161,7 +161,11 @@ inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const K
 // among them until their results are joined.  Per tile a wave forms S^T = K Q^T (keys along the rows: a lane holds eight scores of ONE
 // query row, so the softmax needs no exchange until a reference has to move), P^T stays in the registers in which the second
 // product wants it, and V, which that product wants with the keys side by side, is read from its rows by transposing LDS reads.
-// Reading every key and value once bounds it for up to about 64 query rows.
+// Bytes bound it for up to about 64 query rows: 48 tokens over up to 9000 keys of 32 / 8 heads of 64 take 105 us (5.2 TB/s), 3 over 131072 143 us (5.6).  With more, it is the chain of a tile (its reads from LDS,
+// the two products, the softmax between them), which the two or three workgroups of a compute unit hide in part: 16 trees of 64 rows
+// over 4000 keys 72 us (470 TFLOP/s), chains of 300 rows, head size 128, 104 us (580).
+// Only row blocks that exist are units: a batch's sequences have one row or hundreds (us, units of the longest sequence's blocks for all / these: 16 trees
+// of up to 64 rows 57 / 39, of up to 48 with 24 / 8 heads of 128 79 / 67, 8 chains of up to 300 158 / 145).
 constexpr int KA_WAVES = 4;
 constexpr int KA_STEP = 128;              // keys are cut into slots at multiples of this
 constexpr int KA_CUS = 256;               // compute units
@@ -169,7 +173,9 @@ constexpr int KA_PLANNED = 1024;          // sequences up to which long ones are
 constexpr int KA_FEW = 512;               // keys of a sequence up to which the probabilities are not rounded
 constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
 
-struct KvSeq { int s, len, row0, rows, all, total, first, last, count, slot0; };   // keys of a slot: [first, last)
+// A workgroup's unit: keys [first, last) of a sequence, the slot-th of `count` runs, and block rb of its query rows, of brows each.  The
+// sequence's units start at unit0: slot by slot, in each of them its row blocks.
+struct KvSeq { int s, len, row0, rows, all, total, first, last, count, slot, blocks, brows, rb, unit0; };
 
 // Sum over the lanes up to this one.
 __device__ __forceinline__ int wave_scan(int v) {
@@ -184,11 +190,12 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
-// The sequence and keys of slot w.  A sequence of n steps (of `step` keys) has ceil(n / per) slots of equal length, at least one; `per` is the
-// least number for which all slots fit in n_seqs + spare.  All lanes of a wave work it out together, 64 sequences at a time.
-__device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int w, int spare, int step, KvSeq& q) {
+// Unit w.  A sequence of n steps (of `step` keys) has ceil(n / per) slots of equal length, at least one, and each of them one unit per block of at most
+// `most` query rows; `per` is the least number for which all units fit in the row blocks of all sequences + spare.  All lanes of a wave work it out
+// together, 64 sequences at a time.  Without spare ones a sequence has `blocks` units, alive or not.
+__device__ __forceinline__ bool kv_find_unit(const KvView& c, int max_rows, int group, int w, int spare, int blocks, int most, int step, KvSeq& q) {
   const int lane = threadIdx.x & 63;
-  int len, row0, rows, all, total, steps;
+  int len, row0, rows, all, total, steps, live;
   auto load = [&](int s) __attribute__((always_inline)) {
     const int64_t cap = (int64_t)c.max_pages << c.page_shift;
     len = c.lens[s];
@@ -199,36 +206,45 @@ __device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int 
     rows = min(all, max_rows);
     total = (int)min((int64_t)len + rows, cap);
     steps = rows > 0 ? (total + step - 1) / step : 0;
+    live = max(1, (int)((unsigned)(rows * group + most - 1) / (unsigned)most));
   };
-  int s = w, slot0 = w, count = 1;
+  int s, unit0, count = 1;
   if (spare == 0) {                        // one slot per sequence
-    if (w >= c.n_seqs) return false;
-    load(w);
+    s = w / blocks;
+    if (s >= c.n_seqs) return false;
+    load(s);
+    unit0 = s * blocks;
   } else {
     int64_t sum = 0;
+    int least = 0;                         // units of uncut sequences
     for (int b = 0; b < c.n_seqs; b += 64) {
       load(min(b + lane, c.n_seqs - 1));
-      sum += __builtin_amdgcn_readlane(wave_scan(b + lane < c.n_seqs ? steps : 0), 63);
+      const bool in = b + lane < c.n_seqs;
+      const int64_t n = in ? min((int64_t)steps * live, (int64_t)1 << 36) : 0;       // (a wave's sum may pass 32 bits)
+      sum += ((int64_t)__builtin_amdgcn_readlane(wave_scan((int)(n >> 20)), 63) << 20) + __builtin_amdgcn_readlane(wave_scan((int)(n & 0xfffff)), 63);
+      least += __builtin_amdgcn_readlane(wave_scan(in ? live : 0), 63);
     }
     unsigned per = sum > 0x7fff0000 - spare ? 0x7fffffffu : max(1u, ((unsigned)sum + spare - 1) / (unsigned)spare);
-    auto slots_of = [&]() __attribute__((always_inline)) { return steps > 0 ? (int)((unsigned)(steps - 1) / per) + 1 : 1; };
-    // few long sequences: no more slots than `spare`, which fill the chip once (3 x 131072 keys in 264 workgroups of which 8 wait for a second
-    // round: 194 us, in 256: 151; the loop ends: per grows, and n_seqs slots fit)
-    if (c.n_seqs <= 64 && c.n_seqs * 4 <= spare)
-      for (int over; (over = __builtin_amdgcn_readlane(wave_scan(lane < c.n_seqs ? slots_of() : 0), 63) - spare) > 0;)
+    auto units_of = [&]() __attribute__((always_inline)) { return steps > 0 ? ((int)((unsigned)(steps - 1) / per) + 1) * live : 1; };
+    // few long sequences: no more units than `spare`, which fill the chip once (3 x 131072 keys in 264 workgroups of which 8 wait for a second
+    // round: 194 us, in 256: 151; 2 chains of 300 rows over 6000 keys, 32 / 8 heads of 128: 128 and 104).  More of them would be as long as the cut that fits allows: 48 tokens
+    // over up to 9000 keys 106 -> 110.  (The loop ends: per grows, and uncut sequences fit.)
+    if (c.n_seqs <= 64 && least <= spare / 2)
+      for (int over; (over = __builtin_amdgcn_readlane(wave_scan(lane < c.n_seqs ? units_of() : 0), 63) - spare) > 0;)
         per += max(1u, (unsigned)((uint64_t)per * over / (2u * spare)));
     int before = 0;
     s = -1;
     for (int b = 0; b < c.n_seqs; b += 64) {
       if (c.n_seqs > 64) load(min(b + lane, c.n_seqs - 1));
-      const int n = b + lane < c.n_seqs ? slots_of() : 0;
+      const int n = b + lane < c.n_seqs ? units_of() : 0;
       const int upto = wave_scan(n), start = before + upto - n;
       const unsigned long long hit = __ballot(w >= start && w < start + n);
       if (hit) {
         const int l = __ffsll(hit) - 1;
         s = b + l;
-        slot0 = __builtin_amdgcn_readlane(start, l);
-        count = __builtin_amdgcn_readlane(n, l);
+        unit0 = __builtin_amdgcn_readlane(start, l);
+        live = __builtin_amdgcn_readlane(live, l);
+        count = (int)((unsigned)__builtin_amdgcn_readlane(n, l) / (unsigned)live);
         len = __builtin_amdgcn_readlane(len, l);
         row0 = __builtin_amdgcn_readlane(row0, l);
         rows = __builtin_amdgcn_readlane(rows, l);
@@ -242,20 +258,25 @@ __device__ __forceinline__ bool kv_find_slot(const KvView& c, int max_rows, int 
     if (s < 0) return false;
   }
   q.s = __builtin_amdgcn_readfirstlane(s);
-  q.slot0 = __builtin_amdgcn_readfirstlane(slot0);
+  q.unit0 = __builtin_amdgcn_readfirstlane(unit0);
   q.count = __builtin_amdgcn_readfirstlane(count);
   q.len = __builtin_amdgcn_readfirstlane(len);
   q.row0 = __builtin_amdgcn_readfirstlane(row0);
   q.rows = __builtin_amdgcn_readfirstlane(rows);
   q.all = __builtin_amdgcn_readfirstlane(all);
   q.total = __builtin_amdgcn_readfirstlane(total);
+  q.blocks = __builtin_amdgcn_readfirstlane(live);
+  q.brows = ((int)((unsigned)(q.rows * group + q.blocks - 1) / (unsigned)q.blocks) + 15) & ~15;       // evenly over the blocks, at most `most`
+  const unsigned i = w - q.unit0;
+  q.slot = q.count > 1 ? (int)(i / (unsigned)q.blocks) : 0;
+  q.rb = (int)i - q.slot * q.blocks;
   // the first (steps % count) slots take one step more
   q.first = 0;
   q.last = q.total;
   if (q.count > 1) {
-    const unsigned n = __builtin_amdgcn_readfirstlane(steps), i = w - q.slot0, base = n / (unsigned)q.count, more = n - base * q.count;
-    q.first = __builtin_amdgcn_readfirstlane((int)(i * base + min(i, more)) * step);
-    q.last = __builtin_amdgcn_readfirstlane(min(q.first + (int)(base + (i < more)) * step, q.total));
+    const unsigned n = __builtin_amdgcn_readfirstlane(steps), k = q.slot, base = n / (unsigned)q.count, more = n - base * q.count;
+    q.first = __builtin_amdgcn_readfirstlane((int)(k * base + min(k, more)) * step);
+    q.last = __builtin_amdgcn_readfirstlane(min(q.first + (int)(base + (k < more)) * step, q.total));
   }
   return true;
 }
@@ -351,18 +372,17 @@ __device__ __forceinline__ float row_max(float v) {
   return fmaxf(v, __shfl_xor(v, 32, kWave));
 }
 
-// q, out: [n_rows][H dh]; tree: [n_rows] or null; part: [slots][Hkv][prows][DH] and pml: the same rows x {reference in log2,
-// sum} for sequences of more than one slot, whose rows' {first slot, slots, row in the sequence} go to row_slot [n_rows][4].
+// q, out: [n_rows][H dh]; tree: [n_rows] or null; part: [units][Hkv][prows][DH] and pml: the same rows x {reference in log2,
+// sum} for sequences of more than one slot, whose rows' {first unit, slots, row in the sequence, row blocks and their length} go to row_unit [n_rows].
 // SHARED: every wave has 16 QT query rows of its own and all of them read the same tiles, else all have the same rows and tiles of their own.
-// grid: slots Hkv, or 8 ceil(slots Hkv / 8) blocks with more than one row block.  The heads of a slot run side by side: they share its pages (the
-// other way round, 48 sequences took 115 us instead of 107).  Workgroup b belongs to XCD b % 8: row blocks that read the same keys
-// stay on one XCD, one behind the other.
+// grid: units Hkv.  The heads of a unit run side by side: they share its pages (the other way round, 48 sequences took 115 us instead of 107).
+// Workgroup b belongs to XCD b % 8: with eight KV heads the row blocks that read the same keys stay on one XCD, one behind the other.
 template <typename T, int DH, int QT, bool SHARED, int S>
 __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DH == 128 && QT == 2 ? 1 : 2))) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
                                                                const unsigned long long* __restrict__ tree, KvView c,
                                                                T* __restrict__ out, float* __restrict__ part, float* __restrict__ pml,
-                                                               int4* __restrict__ row_slot, int H, int Hkv, int group, int dh, int max_rows,
-                                                               int slots, int spare, int blocks, int brows, float scale_log2e) {
+                                                               int4* __restrict__ row_unit, int H, int Hkv, int group, int dh, int max_rows,
+                                                               int spare, int blocks, int prows, float scale_log2e) {
   typedef KvTile<T, DH> L;
   constexpr int NW = KA_WAVES;
   constexpr bool BF = L::BF;
@@ -372,19 +392,13 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
   static_assert(NCOPY * (SHARED ? NW : 1) == 2 * L::COPIES, "every wave issues the same number of copies");
   extern __shared__ __align__(16) unsigned char smem[];      // rings of S stages; then (not SHARED) [waves][ROWS][DH] fp32 and [waves][ROWS][2]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int pair = blockIdx.x, rb = 0;
-  if (blocks > 1) {
-    const int x = pair >> 3;
-    rb = x % blocks;
-    pair = (x / blocks) * 8 + (pair & 7);
-  }
-  const int w = pair / Hkv, kvh = pair - w * Hkv;
-  if (w >= slots) return;
+  const int w = blockIdx.x / (unsigned)Hkv, kvh = blockIdx.x - w * Hkv;
   KvSeq sq;
-  if (!kv_find_slot(c, max_rows, w, spare, KA_STEP, sq)) return;
-  if (spare && kvh == 0 && rb == 0 && w == sq.slot0)
-    for (int i = threadIdx.x; i < sq.all; i += NW * 64) row_slot[sq.row0 + i] = make_int4(w, i < sq.rows ? sq.count : 0, i, 0);
-  const int q0 = rb * brows, nq = min(sq.rows * group, q0 + brows);       // query rows of the workgroup: [q0, nq)
+  if (!kv_find_unit(c, max_rows, group, w, spare, blocks, ROWS * (SHARED ? NW : 1), KA_STEP, sq)) return;
+  if (spare && kvh == 0 && w == sq.unit0)
+    for (int i = threadIdx.x; i < sq.all; i += NW * 64)
+      row_unit[sq.row0 + i] = make_int4(w, i < sq.rows ? sq.count : 0, i, sq.blocks << 8 | sq.brows);
+  const int q0 = sq.rb * sq.brows, nq = min(sq.rows * group, q0 + sq.brows);       // query rows of the workgroup: [q0, nq)
   if (q0 >= nq) return;
   // 16-row tile t of a wave: waves that share the keys take the block's tiles in turn, so that a short block is spread over them
   auto qtile = [&](int t) __attribute__((always_inline)) { return q0 + (SHARED ? t * NW + wave : t) * 16; };
@@ -701,7 +715,7 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
       for (int e = 0; e < 4; ++e) v4.v[e] = from_f32<T>(ref == -INFINITY ? 0.f : acc[e] * inv);
       *(Pack<T, 4>*)(out + (int64_t)(sq.row0 + i) * (H * dh) + (kvh * group + g) * dh + d) = v4;
     } else {
-      const int64_t at = ((int64_t)w * Hkv + kvh) * (blocks * brows) + qi;
+      const int64_t at = ((int64_t)w * Hkv + kvh) * prows + qi - q0;
       *(f32x4*)(part + at * DH + d) = acc;
       if (d == 0) { pml[at * 2] = ref; pml[at * 2 + 1] = sum; }
     }
@@ -759,18 +773,20 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
 // row, so 64 / (DH / 4) slots are read at a time.  grid: ceil(n_rows H / 4), block: 256.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, T* __restrict__ out, const float* __restrict__ part, const float* __restrict__ pml,
-                                                      const int4* __restrict__ row_slot, int H, int Hkv, int dh, int max_rows, int slots, int prows) {
+                                                      const int4* __restrict__ row_unit, int H, int Hkv, int dh, int max_rows, int units, int prows) {
   constexpr int LANES = DH / 4, TOGETHER = 64 / LANES;
   const int lane = threadIdx.x & 63, sub = lane / LANES, d = lane % LANES * 4, group = H / Hkv;
   const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), row = x / H;
   const int h = (int)(x - row * H), kvh = h / group;
   if (row >= c.n_rows) return;
-  const int4 rs = row_slot[row];
-  // rows outside [row_start[0], row_start[n_seqs]) are nobody's, and nobody has written their entry; no entry leads outside the slots
+  const int4 ru = row_unit[row];
+  // rows outside [row_start[0], row_start[n_seqs]) are nobody's, and nobody has written their entry; no entry leads outside the units
   if (row < c.row_start[0] || row >= c.row_start[c.n_seqs]) return;
-  const int slot = rs.x, count = rs.y, i = rs.z;
-  if (count <= 1 || slot < 0 || count > slots - slot || i < 0 || i >= max_rows) return;
-  const int64_t at0 = ((int64_t)slot * Hkv + kvh) * prows + i * group + (h - kvh * group), step = (int64_t)Hkv * prows;
+  const int unit0 = ru.x, count = ru.y, i = ru.z, blocks = ru.w >> 8, brows = ru.w & 255;
+  if (count <= 1 || unit0 < 0 || blocks < 1 || (int64_t)unit0 + (int64_t)count * blocks > units || i < 0 || i >= max_rows || brows < 16 || brows > prows) return;
+  const int qi = i * group + (h - kvh * group), rb = (int)((unsigned)qi / (unsigned)brows);
+  if (rb >= blocks) return;
+  const int64_t at0 = ((int64_t)(unit0 + rb) * Hkv + kvh) * prows + qi - rb * brows, step = (int64_t)blocks * Hkv * prows;
   float ref = -INFINITY;
   for (int n = lane; n < count; n += 64) ref = fmaxf(ref, pml[(at0 + n * step) * 2]);
   float sum = 0.f;
@@ -802,9 +818,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvView c, T* __restrict__ 
 
 // Shape of a launch, from what the host knows (the lengths are on the device).
 struct KvPlan {
-  int DH, QT, blocks, brows, slots, spare;
+  int DH, QT, blocks, prows, units, spare;
   bool shared;
-  size_t part, pml, row_slot, total;         // workspace
+  size_t part, pml, row_unit, total;         // workspace
 };
 
 inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max_keys, int H, int Hkv, int dh, int target = 0) {
@@ -814,18 +830,16 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   p.QT = nq <= 16 ? 1 : nq <= 32 || p.DH == 128 || !bf ? 2 : 4;
   p.shared = bf && nq > 16 * p.QT;
   if (p.shared) p.QT = p.DH == 128 && nq <= 64 ? 1 : 2;
-  // rows of a block: no more than its waves hold, and evenly over the blocks
-  const int rows = 16 * p.QT * (p.shared ? KA_WAVES : 1);
-  p.blocks = (int)((nq + rows - 1) / rows);
-  p.brows = (int)(((nq + p.blocks - 1) / p.blocks + 15) / 16 * 16);
+  const int most = 16 * p.QT * (p.shared ? KA_WAVES : 1);       // rows of a block
+  p.blocks = (int)((nq + most - 1) / most);
+  p.prows = (int)(nq < most ? (nq + 15) / 16 * 16 : most);
+  // row blocks of all sequences: those that hold n_rows, and a partial one each
+  const int64_t every = (int64_t)n_seqs * p.blocks, held = n_seqs + (int64_t)n_rows * (H / Hkv) / most, least = every < held ? every : held;
   const int64_t steps = (max_keys + KA_STEP - 1) / KA_STEP;
   // workgroups wanted: what the chip holds at once
   const int resident = p.shared ? (p.DH == 64 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
-  int64_t spare = (target ? target : KA_CUS * resident) / ((int64_t)Hkv * p.blocks);
-  // ... and twice that where many sequences of 128 dimensions share it (a workgroup's walk is longest there, and uneven): 16 trees of up to 48 drafts of 24 / 8
-  // heads 90 -> 77 us, 32 of 16 of 32 / 8 70.7 -> 64.2; two chains of 300 rows 101 -> 110, at 64 dimensions no better
-  if (p.shared && p.DH == 128 && n_seqs >= 8 && n_seqs * 4 > spare) spare *= 2;
-  if (spare > n_seqs * (steps - 1)) spare = n_seqs * (steps - 1);         // cuts that keys could be made at
+  int64_t spare = (target ? target : KA_CUS * resident) / Hkv;
+  if (spare > least * (steps - 1)) spare = least * (steps - 1);         // cuts that keys could be made at
   // Short caches of one row tile are not cut: a second launch costs more than the walk through ten steps, sixteen where the workgroups are
   // many (us, cut and joined / whole: 1 x 1040 keys 6.4 + 3.8 / 9.9, 1 x 2000 7.2 + 3.8 / 13.4, 8 x 2000 11.5 + 4.0 / 14.2, 32 x 2000 27.1 + 4.8 / 27.6)
   if (!p.shared && p.QT == 1 && (steps <= 10 || (steps <= 16 && (int64_t)n_seqs * Hkv * p.blocks >= 64))) spare = 0;
@@ -833,19 +847,18 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   // 520 125 / 299, 1024 270 / 322, 4096 2549 / 501; 1024 with eight of 20000 304 / 258)
   if (n_seqs > KA_PLANNED) spare = 0;
   p.spare = (int)(spare < 0 ? 0 : spare);
-  p.slots = n_seqs + p.spare;
+  p.units = (int)(p.spare ? least + p.spare : every < 0x7fffffff ? every : 0x7fffffff);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  const size_t all = p.spare ? (size_t)p.slots * Hkv * p.blocks * p.brows : 0;
+  const size_t all = p.spare ? (size_t)p.units * Hkv * p.prows : 0;
   p.part = 0;
   p.pml = up(all * p.DH * 4);
-  p.row_slot = p.pml + up(all * 8);
-  p.total = p.row_slot + (p.spare ? up((size_t)n_rows * 16) : 0);
+  p.row_unit = p.pml + up(all * 8);
+  p.total = p.row_unit + (p.spare ? up((size_t)n_rows * 16) : 0);
   return p;
 }
 
 inline int64_t kv_grid(const KvPlan& p, int Hkv) {
-  const int64_t pairs = (int64_t)p.slots * Hkv;
-  return p.blocks == 1 ? pairs : 8 * ((pairs + 7) / 8) * p.blocks;
+  return (int64_t)p.units * Hkv;
 }
 
 template <typename T, int DH, int QT, bool SHARED, int S>
@@ -860,13 +873,13 @@ hipError_t launch_kv_attention_as(const KvPlan& p, const void* q, const void* k,
   }
   const unsigned grid = (unsigned)kv_grid(p, Hkv);
   float *part = (float*)(ws + p.part), *pml = (float*)(ws + p.pml);
-  int4* row_slot = (int4*)(ws + p.row_slot);
+  int4* row_unit = (int4*)(ws + p.row_unit);
   kv_attention_kernel<T, DH, QT, SHARED, S><<<grid, KA_WAVES * 64, lds, st>>>(
-      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, part, pml, row_slot, H, Hkv, H / Hkv, dh, max_rows, p.slots, p.spare, p.blocks, p.brows,
+      (const T*)q, (const T*)k, (const T*)v, tree, c, (T*)out, part, pml, row_unit, H, Hkv, H / Hkv, dh, max_rows, p.spare, p.blocks, p.prows,
       1.4426950408889634f / sqrtf((float)dh));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.spare) return e;
-  kv_join_kernel<T, DH><<<(unsigned)(((int64_t)c.n_rows * H + 3) / 4), 256, 0, st>>>(c, (T*)out, part, pml, row_slot, H, Hkv, dh, max_rows, p.slots, p.blocks * p.brows);
+  kv_join_kernel<T, DH><<<(unsigned)(((int64_t)c.n_rows * H + 3) / 4), 256, 0, st>>>(c, (T*)out, part, pml, row_unit, H, Hkv, dh, max_rows, p.units, p.prows);
   return hipGetLastError();
 }
 

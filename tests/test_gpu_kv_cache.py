@@ -119,6 +119,12 @@ ATTEND = [
     ("eight", "f32", 16, [130, 0], [20, 1], False),
     ("twelve", "f32", 32, [31, 64], [4, 1], True),
     ("eight", "f32", 16, [s % 90 for s in range(600)], [s % 3 for s in range(600)], False),
+    # rows of one sequence in several blocks, next to single ones, all of them cut
+    ("8b", "bf16", 64, [2000, 5, 700, 2500], [1, 200, 40, 0], False),
+    ("3b", "bf16", 16, [900, 1300, 0, 640, 1500], [60, 1, 33, 64, 44], True),
+    ("1b", "f32", 64, [1700, 10, 600], [60, 1, 3], False),
+    ("160m", "bf16", 64, [1500, 2, 900], [150, 300, 1], False),
+    ("one", "bf16", 32, [s * 37 % 1400 for s in range(70)], [s * s % 21 for s in range(70)], False),
 ]
 
 
