@@ -363,7 +363,7 @@ armt_status armt_kv_append(const armt_config *cfg, const armt_kv_cache *cache, c
  * What a row does not see has no influence on it, not even a NaN; a row that sees no key is zero.  max_rows: at least the
  * rows of any sequence (a longer sequence's further rows are left as they are).  Scores, probabilities' sums and outputs are
  * accumulated in fp32; in bf16 the probabilities are rounded to bf16 for the second product where a sequence has more than 512 keys and
- * max_rows * H / Hkv > 16.  The workspace is
+ * more than 64 Hkv / H rows.  The workspace is
  * armt_kv_attention_workspace_bytes (0 = rejected) and 256-byte aligned; calls that may overlap need one each. */
 size_t armt_kv_attention_workspace_bytes(const armt_config *cfg, int32_t n_seqs, int32_t max_pages, int32_t page_len, int32_t n_rows,
                                          int32_t max_rows);

@@ -165,12 +165,12 @@ inline hipError_t launch_kv_append(bool bf, const void* qkv, int64_t ld, const K
 // the two products, the softmax between them), which the two or three workgroups of a compute unit hide in part: 16 trees of 64 rows
 // over 4000 keys 72 us (470 TFLOP/s), chains of 300 rows, head size 128, 104 us (580).
 // Only row blocks that exist are units: a batch's sequences have one row or hundreds (us, units of the longest sequence's blocks for all / these: 16 trees
-// of up to 64 rows 57 / 39, of up to 48 with 24 / 8 heads of 128 79 / 67, 8 chains of up to 300 158 / 145).
+// of up to 64 rows 57 / 39, of up to 48 with 24 / 8 heads of 128 79 / 67 (59 by now), 8 chains of up to 300 158 / 145).
 constexpr int KA_WAVES = 4;
 constexpr int KA_STEP = 128;              // keys are cut into slots at multiples of this
 constexpr int KA_CUS = 256;               // compute units
 constexpr int KA_PLANNED = 1024;          // sequences up to which long ones are cut: every workgroup looks at all lengths
-constexpr int KA_FEW = 512;               // keys of a sequence up to which the probabilities are not rounded
+constexpr int KA_FEW = 512, KA_FEW_ROWS = 64;      // keys and query rows of a sequence up to which the probabilities are not rounded
 constexpr float KA_LAZY_SUM = 4096.f;     // unnormalised probabilities of a lane's keys of a tile may add up to this before the reference moves
 
 // A workgroup's unit: keys [first, last) of a sequence, the slot-th of `count` runs, and block rb of its query rows, of brows each.  The
@@ -378,7 +378,7 @@ __device__ __forceinline__ float row_max(float v) {
 // grid: units Hkv.  The heads of a unit run side by side: they share its pages (the other way round, 48 sequences took 115 us instead of 107).
 // Workgroup b belongs to XCD b % 8: with eight KV heads the row blocks that read the same keys stay on one XCD, one behind the other.
 template <typename T, int DH, int QT, bool SHARED, int S>
-__global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DH == 128 && QT == 2 ? 1 : 2))) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
+__global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DH == 128 && QT == 2 ? 1 : SHARED && DH == 128 && QT == 1 ? 3 : 2))) void kv_attention_kernel(const T* __restrict__ q, const T* __restrict__ kc, const T* __restrict__ vc,
                                                                const unsigned long long* __restrict__ tree, KvView c,
                                                                T* __restrict__ out, float* __restrict__ part, float* __restrict__ pml,
                                                                int4* __restrict__ row_unit, int H, int Hkv, int group, int dh, int max_rows,
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
 
   bool any_odd = false;       // values that are not finite were left out
   const int whole_until = min(sq.len, last);
-  const bool few_keys = sq.total <= KA_FEW;
+  const bool exact_p = sq.total <= KA_FEW || sq.rows * group <= KA_FEW_ROWS;
   auto tile = [&](int it, int stage, int pages_ok) __attribute__((always_inline)) {
     unsigned char* Kt = (unsigned char*)ring + stage * STAGE;
     unsigned char* Vt = Kt + L::BYTES;
@@ -611,8 +611,9 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
       }
       lsum[t] += hs;
       if constexpr (BF) {
-        // P in bf16, as the operand of the matrix product: half a step of 2^-8 each.  Where the keys' bytes are what takes time (one row tile: 48 sequences
-        // 106 us with and without) and where keys are few, so that single roundings show, what they leave follows as a second operand.
+        // P in bf16, as the operand of the matrix product: half a step of 2^-8 each.  Where the keys' bytes are what takes time (up to 64 query rows:
+        // 48 tokens 106 us with and without, 16 trees of 8 drafts with 32 / 8 heads of 128 61 and 61, of 16 with heads of 64 42 and 43) and where keys are few, so that single
+        // roundings show, what they leave follows as a second operand.  (In a chain of 300 rows that would cost 14 %.)
         bf16x8 pf;
 #pragma unroll
         for (int a = 0; a < 2; ++a)
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
           for (int r = 0; r < 4; ++r) pf[a * 4 + r] = (bf16)pr[a][r];
 #pragma unroll
         for (int d = 0; d < NT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
-        if ((QT == 1 && !SHARED) || few_keys) {
+        if ((QT == 1 && !SHARED) || exact_p) {
 #pragma unroll
           for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -829,7 +830,10 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   const int64_t nq = (int64_t)max_rows * (H / Hkv);
   p.QT = nq <= 16 ? 1 : nq <= 32 || p.DH == 128 || !bf ? 2 : 4;
   p.shared = bf && nq > 16 * p.QT;
-  if (p.shared) p.QT = p.DH == 128 && nq <= 64 ? 1 : 2;
+  // 128 dimensions: two row tiles take a wave 254 registers, one 146, so that three workgroups share a compute unit.  For few row blocks that is worth more than
+  // reading their keys less often (us, two / one: 16 trees of up to 48 rows, 24 / 8 heads, 67 / 59, 32 / 8 heads: 16 of up to 32 87 / 82, 40 of up to 24 92 / 88, 16 of 20 69 / 70, 32 chains of 32
+  // 110 / 118; more rows, 8 chains of 64 105 / 110, 2 of 300 105 / 118)
+  if (p.shared) p.QT = p.DH == 128 && nq <= 192 ? 1 : 2;
   const int most = 16 * p.QT * (p.shared ? KA_WAVES : 1);       // rows of a block
   p.blocks = (int)((nq + most - 1) / most);
   p.prows = (int)(nq < most ? (nq + 15) / 16 * 16 : most);
@@ -837,7 +841,7 @@ inline KvPlan kv_plan(bool bf, int n_seqs, int n_rows, int max_rows, int64_t max
   const int64_t every = (int64_t)n_seqs * p.blocks, held = n_seqs + (int64_t)n_rows * (H / Hkv) / most, least = every < held ? every : held;
   const int64_t steps = (max_keys + KA_STEP - 1) / KA_STEP;
   // workgroups wanted: what the chip holds at once
-  const int resident = p.shared ? (p.DH == 64 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
+  const int resident = p.shared ? (p.DH == 64 || p.QT == 1 ? 3 : 2) : p.DH == 32 ? 4 : p.DH == 64 ? 2 : 1;       // (registers; 1 KB x DH of rings in 160 KB of LDS)
   int64_t spare = (target ? target : KA_CUS * resident) / Hkv;
   if (spare > least * (steps - 1)) spare = least * (steps - 1);         // cuts that keys could be made at
   // Short caches of one row tile are not cut: a second launch costs more than the walk through ten steps, sixteen where the workgroups are
@@ -888,7 +892,7 @@ inline hipError_t launch_kv_attention(bool bf, const KvPlan& p, const void* q, c
 #define ARMT_KA(T, D, Q, SH, S) return launch_kv_attention_as<T, D, Q, SH, S>(p, q, k, v, tree, c, out, ws, H, Hkv, dh, max_rows, st)
   if (bf && p.shared) {
     if (p.DH == 64) ARMT_KA(bf16, 64, 2, true, 4);
-    if (p.QT == 1) ARMT_KA(bf16, 128, 1, true, 4);
+    if (p.QT == 1) ARMT_KA(bf16, 128, 1, true, 3);
     ARMT_KA(bf16, 128, 2, true, 4);
   }
   if (bf) {

@@ -104,7 +104,7 @@ class Problem:
         for s in range(len(self.lens)):
             k, v, have = self.keys_of(s)
             half = HALF_STEP[self.dt]
-            half_p = 0 if self.dt == torch.float32 else half * half if called * H // Hkv <= 16 or len(have) <= 512 else half
+            half_p = 0 if self.dt == torch.float32 else half * half if min(self.rows[s], called) * H // Hkv <= 64 or len(have) <= 512 else half
             for i in range(self.rows[s] if max_rows is None else min(self.rows[s], max_rows)):
                 r = int(self.row_start[s]) + i
                 see = have.clone()
