@@ -563,13 +563,20 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
 #pragma unroll
       for (int a = 0; a < NS; ++a) {
         sc[a] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (BF) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if constexpr (BF) sc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[a][ks], qf[t][ks], sc[a], 0, 0, 0);
-          else {
+          for (int ks = 0; ks < KS; ++ks) sc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[a][ks], qf[t][ks], sc[a], 0, 0, 0);
+        } else {                         // (two short sums round less than a long one)
+          f32x4 odd = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[a][ks][e], qf[t][ks][e], sc[a], 0, 0, 0);
-          }
+          for (int ks = 0; ks < KS; ks += 2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              sc[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[a][ks][e], qf[t][ks][e], sc[a], 0, 0, 0);
+              odd = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[a][ks + 1][e], qf[t][ks + 1][e], odd, 0, 0, 0);
+            }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[a][r] += odd[r];
         }
       }
       if (edge) {
@@ -630,10 +637,15 @@ __global__ __launch_bounds__(KA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(s
           for (int d = 0; d < NT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], pf, o[t][d], 0, 0, 0);
         }
       } else {
+        // a tile's 16 keys first, then the tiles: one sum over all keys would round as often as there are keys
 #pragma unroll
-        for (int d = 0; d < NT; ++d)
+        for (int d = 0; d < NT; ++d) {
+          f32x4 of = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[(d / 4) * 4 + r][d % 4], pr[0][r], o[t][d], 0, 0, 0);
+          for (int r = 0; r < 4; ++r) of = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[(d / 4) * 4 + r][d % 4], pr[0][r], of, 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[t][d][r] += of[r];
+        }
       }
     }
   };
